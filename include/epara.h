@@ -837,6 +837,209 @@ typedef struct {
  * not 16-byte aligned). */
 int32_t epara_attention(const epara_attn_args* h_args, const epara_attn_args* d_args, int32_t G, void* stream);
 
+/* ---- device side: between the dense layers of a decoder block ------------------------------ */
+
+/* The co-located language-model services (the decode and prefill mixes) run, per decoder block, normalisation -> QKV
+ * projection -> rotary positions and the cache -> attention over the cache -> output projection -> normalisation ->
+ * SwiGLU FFN; the projections and the FFN are grouped dense forwards, and the calls below are what lies between
+ * them, each for all services in one call.  None allocates device memory or synchronises. */
+
+/* Rows of one service through a residual connection and a root-mean-square normalisation (Zhang and Sennrich 2019):
+ * s = x + r per element (r absent: s = x), then per row of d values y = s / sqrt(mean(s^2) + eps) * gamma.  The
+ * statistic and y come from the unrounded fp32 sum; S receives the sum rounded to bf16.  Y is bf16, or E4M3 codes:
+ *   row_scales given: a row's scale is max |y| / 448 (1 for a row of zeros), code = sat(RNE(y * (1 / scale)));
+ *   row_scales NULL:  code = sat(RNE(y * out_inv_scale)), the service's static scale: what a grouped forward with
+ *                     scale = s_x * s_w reads.
+ * A row that holds a NaN or an infinity gets unspecified codes and a scale that is not finite.  72 bytes. */
+typedef struct {
+    const void*  X;              /* device, bf16 [M, d] row-major, 16-byte aligned */
+    const void*  R;              /* device, bf16 [M, d], or NULL */
+    const float* gamma;          /* device, fp32 [d], 16-byte aligned */
+    void*        S;              /* device, bf16 [M, d], or NULL (the sum is not kept); may be the same buffer as X or R */
+    void*        Y;              /* device, [M, d] in out_dtype, 16-byte aligned; bf16: may be X or R when S is not the same buffer */
+    float*       row_scales;     /* device, fp32 [M], or NULL; EPARA_FP8_E4M3 only */
+    int32_t      M, d;           /* M >= 0; d a multiple of 8, 8 <= d <= EPARA_NORM_MAX_D */
+    float        eps;            /* >= 0 */
+    float        out_inv_scale;  /* E4M3 without row_scales: > 0 and finite; else ignored */
+    int32_t      first_row;      /* rows of all earlier groups: the running sum of M */
+    int32_t      reserved;
+} epara_rmsnorm_args;
+
+/* One kernel on `stream`; out_dtype is EPARA_BF16 or EPARA_FP8_E4M3 for the whole call.  G = 0 or no rows enqueues
+ * nothing.  Errors (from h_args): ERR_DTYPE (out_dtype); ERR_NULL (an array missing; X, gamma or Y NULL in a group with rows);
+ * ERR_SHAPE (M < 0, d out of range or not a multiple, eps or a static scale that is not allowed, first_row not the running sum,
+ * row_scales with bf16, Y the same buffer as S, or as X or R in 8 bits, more than 2^31 - 1 rows in all); ERR_ALIGN. */
+int32_t epara_add_rmsnorm(const epara_rmsnorm_args* h_args, const epara_rmsnorm_args* d_args, int32_t G, int32_t out_dtype, void* stream);
+
+/* A paged cache in 8 bits.  A service's cache of one layer is n_pages pages of EPARA_CACHE_PAGE tokens; a page holds, for
+ * each of kv_heads heads, the keys and then the values of its tokens as E4M3 codes (64 * head_dim bytes each), and
+ * `scales` holds four bytes for each (page, head): keys of tokens 0..31, keys of tokens 32..63, values of tokens 0..31,
+ * values of tokens 32..63.  A scale byte b stands for 2^(b - 127) (E8M0), and a code c for e4m3(c) * 2^(b - 127).  Scales are
+ * powers of two because a block that later gets a larger token is then rescaled without a second rounding (but for
+ * codes that become subnormal), and because the matrix cores take such scales as they are.
+ * Inside a page the codes lie as the matrix cores read them, in 16-byte chunks:
+ *   keys:   token t, dims 16 c .. 16 c + 15:   chunk (((t / 4) % 4) * (head_dim / 16) + c) * 16 + 4 * (t / 16) + t % 4
+ *   values: dim d, tokens 16 q .. 16 q + 15:   chunk ((d / 16) * 4 + q) * 16 + d % 16
+ * The tokens of a sequence lie in the pages that its part of the page table names, 64 to a page, in order.  What lies behind a
+ * sequence's last token in its last page is never looked at. */
+#define EPARA_CACHE_PAGE 64
+#define EPARA_CACHE_BLOCK 32
+#define EPARA_CACHE_MAX_GROUP 64          /* query heads to a key head */
+#define EPARA_CACHE_MAX_TOKENS 16777216   /* of one sequence */
+
+/* The new tokens of one sequence in a call: rows first_row .. first_row + rows - 1 of its service's tensors, at the
+ * positions start .. start + rows - 1 of the sequence.  A negative start makes the first -start rows padding in front of the
+ * sequence (batches padded on the left): they join no cache, see no key and get rows of zeros from the attention.
+ * pages[first_page + i] is the sequence's page i; n_pages entries are its own.  24 bytes, the same on host and device. */
+typedef struct {
+    int32_t service;          /* group of the call; never decreases from one sequence to the next */
+    int32_t first_row, rows;  /* rows >= 0 */
+    int32_t start;            /* start + rows <= n_pages * EPARA_CACHE_PAGE */
+    int32_t first_page, n_pages;
+} epara_sequence;
+
+/* What both cache calls are told about the sequences of all services: host copies are validated, device copies read. */
+typedef struct {
+    const epara_sequence* h_seqs;
+    const epara_sequence* d_seqs;
+    const int32_t* h_pages;       /* page table, n_table entries; only entries that a call needs are looked at */
+    const int32_t* d_pages;
+    int32_t n_seqs, n_table;
+} epara_sequence_table;
+
+/* One service's part of epara_cache_append.  88 bytes. */
+typedef struct {
+    const void*    QKV;         /* device, bf16, row r at QKV + r * qkv_stride elements: [heads | kv_heads | kv_heads] * head_dim */
+    void*          Q;           /* device, bf16, row r at Q + r * q_stride: the rotated queries; NULL (only without rotary): queries stay where they are */
+    void*          codes;       /* device, the cache (16-byte aligned) */
+    uint8_t*       scales;      /* device, [n_pages, kv_heads, 4] (4-byte aligned) */
+    const float*   rotary;      /* device, fp32 [n_positions, head_dim / 2, 2]: cos and sin; NULL: nothing is rotated (16-byte aligned) */
+    const int32_t* positions;   /* device, int32 [rows, 3]: a row's position on each axis; NULL: its position in the sequence on all of them */
+    int32_t rows;               /* rows of QKV and Q */
+    int32_t heads, kv_heads;    /* heads a multiple of kv_heads */
+    int32_t head_dim;           /* 64 or 128 */
+    int32_t n_pages;
+    int32_t qkv_stride, q_stride;   /* multiples of 8 */
+    int32_t n_positions;
+    int32_t axis_pairs[2];      /* pairs 0 .. a0 - 1 of a head turn by axis 0, the next a1 by axis 1, the others by axis 2 */
+} epara_append_args;
+
+/* The step between a QKV projection and attention, for all new tokens of all services in one kernel:
+ *   - pair (x_i, x_{i + head_dim / 2}) of every query and key becomes (x_i cos - x_j sin, x_j cos + x_i sin), with the table's
+ *     row of the token's position on the pair's axis (Su et al. 2021; several axes for images and video).  A position from
+ *     `positions` outside the table takes its nearest row;
+ *   - queries go to Q in bf16; keys and values join the cache.  The block of 32 tokens that a token joins has the smallest
+ *     exponent e >= -96 with max |x| <= 448 * 2^e over its values of this call, or keeps the one it has where earlier tokens lie in it
+ *     and theirs is larger; where it grows, the earlier tokens' codes are rescaled.  Codes are RNE(x * 2^-e).
+ * A call with the same tokens again leaves the cache as it is.  An infinite value is held as the largest code; a token with a NaN in
+ * a head's key or value is held with a NaN key, and zeros for the NaNs: who sees it gets NaN, nobody else does.
+ * Rotation, maxima and products are fp32.  h_first / d_first: int32[n_seqs + 1] from epara_plan_cache_append (running sums
+ * of the work of the sequences).  No rows: nothing is enqueued.
+ * Errors: ERR_NULL; ERR_SHAPE (a dimension out of range, a stride shorter than a row, rows outside the service's, positions outside
+ * the page table or (without `positions`) the rotary table, a page outside the cache, a page that two sequences of the call write,
+ * sequences not ordered by service, h_first not the plan's); ERR_ALIGN; ERR_CAPACITY (too much work for one grid, or no host memory). */
+int32_t epara_plan_cache_append(const epara_append_args* h_args, int32_t G, const epara_sequence_table* table, int32_t* first);
+int32_t epara_cache_append(const epara_append_args* h_args, const epara_append_args* d_args, int32_t G, const epara_sequence_table* table,
+                           const int32_t* h_first, const int32_t* d_first, void* stream);
+
+/* One service's part of epara_cache_attention.  80 bytes. */
+typedef struct {
+    const void*    Q;           /* device, bf16, row r at Q + r * q_stride elements: heads * head_dim */
+    void*          O;           /* device, bf16, row r at O + r * o_stride; not Q */
+    const void*    codes;       /* device, the cache */
+    const uint8_t* scales;
+    int32_t rows;               /* rows of Q and O */
+    int32_t heads, kv_heads;    /* query head h reads key head h / (heads / kv_heads) */
+    int32_t head_dim;           /* 64 or 128 */
+    int32_t n_pages;
+    int32_t q_stride, o_stride; /* multiples of 8 */
+    int32_t window;             /* 0, or a token sees only itself and the window - 1 tokens before it */
+    float   scale;              /* of the scores: 1 / sqrt(head_dim) as a rule; > 0 */
+    float   softcap;            /* 0, or scores are capped: softcap * tanh(score / softcap) */
+    int32_t reserved[2];
+} epara_cache_attn_args;
+
+/* How a call is cut into work: made by epara_plan_cache_attention from the shapes alone (sequences, heads, windows), so that all layers
+ * of a model share it.  first[0 .. n_seqs] and first[n_seqs + 1 .. 2 n_seqs + 1] are running sums of the workgroups of the sequences
+ * with few and with many rows to a key head. */
+typedef struct {
+    int32_t n_items[2];         /* workgroups with few and with many rows */
+    int32_t part_pages[2];      /* pages to a workgroup: a longer context is cut into parts */
+    int64_t workspace_bytes;    /* 0: nothing is cut */
+} epara_cache_attn_plan;
+
+typedef struct {
+    const epara_cache_attn_args* h_args;
+    const epara_cache_attn_args* d_args;
+    const int32_t* h_first;     /* int32[2 * (n_seqs + 1)] */
+    const int32_t* d_first;
+    void*   d_workspace;        /* 256-byte aligned, zeroed once (epara_workspace_init) before its first call; one call at a time */
+    int64_t workspace_bytes;
+    epara_sequence_table table;
+    epara_cache_attn_plan plan;
+    int32_t G, reserved;
+} epara_cache_attn_launch;
+
+/* Causal attention of new tokens over the cache, in which epara_cache_append has put them: for a row at position p and a query
+ * head, over the keys j <= p (window: and j > p - window) of its sequence
+ *   z_j = scale * q . k_j (capped: softcap * tanh(z_j / softcap)), o = sum_j exp(z_j - m) v_j / sum_j exp(z_j - m), m = max_j z_j.
+ * A row at a negative position gets zeros.  Keys and values stay E4M3 up to the matrix cores: a query (bf16, 8 significant
+ * bits) is taken as the sum of two E4M3 numbers of 4 bits each, exactly (but for what lies under 2^-14 of its head's largest value), and so
+ * is a weight (rounded to 8 bits); sums, maxima and weights' sums are fp32.  One kernel for sequences with few rows to a
+ * key head, one for those with many; a long context is cut into parts that run side by side, and the last of them to end
+ * adds them up in order: results do not depend on timing.
+ * Errors as for epara_cache_append; also ERR_SHAPE for a scale or softcap that is negative or not finite, O the same buffer as Q, or a
+ * plan that is not this call's, ERR_CAPACITY for a workspace that is too small. */
+int32_t epara_plan_cache_attention(const epara_cache_attn_args* h_args, int32_t G, const epara_sequence_table* table, int32_t n_compute_units,
+                                   int32_t* first, epara_cache_attn_plan* plan);
+int32_t epara_cache_attention(const epara_cache_attn_launch* launch, void* stream);
+
+/* Copies of whole pages inside caches: the pages and scales of moves[first_move .. first_move + n_moves) of every cache (the layers of a
+ * service share their moves).  No destination may be another move's source or destination in the same cache.  40 bytes. */
+typedef struct { int32_t src, dst; } epara_page_move;
+typedef struct {
+    void*    codes;
+    uint8_t* scales;
+    int32_t  n_pages, kv_heads, head_dim;
+    int32_t  first_move, n_moves;
+    int32_t  first_chunk;       /* running sum of n_moves * kv_heads over the earlier caches */
+} epara_page_copy;
+
+/* One kernel on `stream`.  Errors: ERR_NULL; ERR_SHAPE (a dimension out of range, a page outside the cache, a destination that is
+ * used twice or is also a source, moves outside the list, first_chunk not the running sum); ERR_ALIGN; ERR_CAPACITY (no host memory). */
+int32_t epara_copy_pages(const epara_page_copy* h_caches, const epara_page_copy* d_caches, int32_t G,
+                         const epara_page_move* h_moves, const epara_page_move* d_moves, int32_t n_moves, void* stream);
+
+/* ---- host side: which page belongs to whom -------------------------------------------------- */
+
+/* The pages of a cache and how many sequences hold each.  The caller owns both arrays. */
+typedef struct {
+    int32_t* refs;          /* [n_pages]: sequences that hold the page; 0: free */
+    int32_t* free_pages;    /* [n_pages]: the first n_free entries are the free pages, taken from the end */
+    int32_t  n_pages, n_free;
+} epara_page_pool;
+
+/* All pages free; page 0 is the first to be taken.  ERR_NULL, ERR_SHAPE (n_pages < 0). */
+int32_t epara_page_pool_init(epara_page_pool* pool, int32_t* refs, int32_t* free_pages, int32_t n_pages);
+
+/* Takes n pages with one holder each into pages[0 .. n).  ERR_CAPACITY (and nothing taken) if fewer are free. */
+int32_t epara_pages_take(epara_page_pool* pool, int32_t n, int32_t* pages);
+
+/* A second sequence that begins like one of `tokens` tokens in `pages`: child[i] is its page i for all ceil(tokens / 64) of them.  Whole
+ * pages are shared (one holder more); a part-filled last page, which both will write, is a fresh one and *n_moves = 1 with the
+ * copy that epara_copy_pages has to make in moves[0]; otherwise *n_moves = 0.  ERR_CAPACITY (and nothing changed) if no page is free
+ * for it; ERR_SHAPE for pages that nobody holds. */
+int32_t epara_pages_fork(epara_page_pool* pool, const int32_t* pages, int32_t tokens, int32_t* child, epara_page_move* move, int32_t* n_moves);
+
+/* One holder less for each of pages[0 .. n); a page without holders is free again.  Entries of -1 (pages that a window has
+ * left behind) are passed over.  ERR_SHAPE (and nothing changed) for a page that nobody holds, or that is named more often than it is held. */
+int32_t epara_pages_free(epara_page_pool* pool, const int32_t* pages, int32_t n);
+
+/* Moves the pages in use to the lowest numbers: moves[0 .. *n_moves) are the copies for epara_copy_pages (no destination is a
+ * source), and every entry of table[0 .. n_table) (all sequences' pages, -1 passed over) is renamed.  ERR_CAPACITY (and nothing changed; *n_moves
+ * is still written) if there are more than `cap` moves; ERR_SHAPE for an entry that nobody holds. */
+int32_t epara_pages_compact(epara_page_pool* pool, int32_t* table, int32_t n_table, epara_page_move* moves, int32_t cap, int32_t* n_moves);
+
 const char* epara_status_string(int32_t status);
 
 #ifdef __cplusplus

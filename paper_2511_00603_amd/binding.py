@@ -39,6 +39,21 @@ ATTN_ARGS = np.dtype([("QKV", "<u8"), ("O", "<u8"), ("M", "<i4"), ("tokens", "<i
                       ("first_item", "<i4"), ("reserved", "<i4")])
 assert NORM_ARGS.itemsize == 64 and ATTN_ARGS.itemsize == 40
 EPARA_NORM_MAX_D, EPARA_ATTN_MAX_TOKENS, EPARA_ATTN_HEAD_DIM = 8192, 224, 64
+RMSNORM_ARGS = np.dtype([("X", "<u8"), ("R", "<u8"), ("gamma", "<u8"), ("S", "<u8"), ("Y", "<u8"), ("row_scales", "<u8"),
+                         ("M", "<i4"), ("d", "<i4"), ("eps", "<f4"), ("out_inv_scale", "<f4"), ("first_row", "<i4"), ("reserved", "<i4")])
+SEQUENCE = np.dtype([("service", "<i4"), ("first_row", "<i4"), ("rows", "<i4"), ("start", "<i4"), ("first_page", "<i4"), ("n_pages", "<i4")])
+APPEND_ARGS = np.dtype([("QKV", "<u8"), ("Q", "<u8"), ("codes", "<u8"), ("scales", "<u8"), ("rotary", "<u8"), ("positions", "<u8"),
+                        ("rows", "<i4"), ("heads", "<i4"), ("kv_heads", "<i4"), ("head_dim", "<i4"), ("n_pages", "<i4"),
+                        ("qkv_stride", "<i4"), ("q_stride", "<i4"), ("n_positions", "<i4"), ("axis_pairs", "<i4", (2,))])
+CACHE_ATTN_ARGS = np.dtype([("Q", "<u8"), ("O", "<u8"), ("codes", "<u8"), ("scales", "<u8"),
+                            ("rows", "<i4"), ("heads", "<i4"), ("kv_heads", "<i4"), ("head_dim", "<i4"), ("n_pages", "<i4"),
+                            ("q_stride", "<i4"), ("o_stride", "<i4"), ("window", "<i4"), ("scale", "<f4"), ("softcap", "<f4"), ("reserved", "<i4", (2,))])
+PAGE_MOVE = np.dtype([("src", "<i4"), ("dst", "<i4")])
+PAGE_COPY = np.dtype([("codes", "<u8"), ("scales", "<u8"), ("n_pages", "<i4"), ("kv_heads", "<i4"), ("head_dim", "<i4"),
+                      ("first_move", "<i4"), ("n_moves", "<i4"), ("first_chunk", "<i4")])
+assert RMSNORM_ARGS.itemsize == 72 and SEQUENCE.itemsize == 24 and APPEND_ARGS.itemsize == 88 and CACHE_ATTN_ARGS.itemsize == 80
+assert PAGE_MOVE.itemsize == 8 and PAGE_COPY.itemsize == 40
+EPARA_CACHE_PAGE, EPARA_CACHE_BLOCK, EPARA_CACHE_MAX_GROUP, EPARA_CACHE_MAX_TOKENS = 64, 32, 64, 16777216
 EPARA_TABLE_BLOCK = 2
 SIM_REQUEST = np.dtype([("arrival_us", "<i8"), ("slo_us", "<i8"), ("service", "<i4"), ("origin", "<i4"), ("frames", "<i4"), ("fps_milli", "<i4")])
 assert SIM_REQUEST.itemsize == 32
@@ -78,6 +93,33 @@ class Launch(ctypes.Structure):
 
 
 assert ctypes.sizeof(Launch) == 88
+
+
+class SequenceTable(ctypes.Structure):
+    """struct epara_sequence_table."""
+    _fields_ = [("h_seqs", ctypes.c_void_p), ("d_seqs", ctypes.c_void_p), ("h_pages", ctypes.c_void_p), ("d_pages", ctypes.c_void_p),
+                ("n_seqs", ctypes.c_int32), ("n_table", ctypes.c_int32)]
+
+
+class CacheAttnPlan(ctypes.Structure):
+    """struct epara_cache_attn_plan."""
+    _fields_ = [("n_items", ctypes.c_int32 * 2), ("part_pages", ctypes.c_int32 * 2), ("workspace_bytes", ctypes.c_int64)]
+
+
+class CacheAttnLaunch(ctypes.Structure):
+    """struct epara_cache_attn_launch."""
+    _fields_ = [("h_args", ctypes.c_void_p), ("d_args", ctypes.c_void_p), ("h_first", ctypes.c_void_p), ("d_first", ctypes.c_void_p),
+                ("d_workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64), ("table", SequenceTable), ("plan", CacheAttnPlan),
+                ("G", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class PagePool(ctypes.Structure):
+    """struct epara_page_pool."""
+    _fields_ = [("refs", ctypes.c_void_p), ("free_pages", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("n_free", ctypes.c_int32)]
+
+
+assert ctypes.sizeof(SequenceTable) == 40 and ctypes.sizeof(CacheAttnPlan) == 24 and ctypes.sizeof(CacheAttnLaunch) == 120
+assert ctypes.sizeof(PagePool) == 24
 
 
 class SimConfig(ctypes.Structure):
@@ -209,6 +251,20 @@ def lib():
         L.epara_add_layernorm.restype = i32
         L.epara_attention.argtypes = [vp, vp, i32, vp]
         L.epara_attention.restype = i32
+        L.epara_add_rmsnorm.argtypes = [vp, vp, i32, i32, vp]
+        L.epara_plan_cache_append.argtypes = [vp, i32, vp, vp]
+        L.epara_cache_append.argtypes = [vp, vp, i32, vp, vp, vp, vp]
+        L.epara_plan_cache_attention.argtypes = [vp, i32, vp, i32, vp, vp]
+        L.epara_cache_attention.argtypes = [vp, vp]
+        L.epara_copy_pages.argtypes = [vp, vp, i32, vp, vp, i32, vp]
+        L.epara_page_pool_init.argtypes = [vp, vp, vp, i32]
+        L.epara_pages_take.argtypes = [vp, i32, vp]
+        L.epara_pages_fork.argtypes = [vp, vp, i32, vp, vp, vp]
+        L.epara_pages_free.argtypes = [vp, vp, i32]
+        L.epara_pages_compact.argtypes = [vp, vp, i32, vp, i32, vp]
+        for name in ("epara_add_rmsnorm", "epara_plan_cache_append", "epara_cache_append", "epara_plan_cache_attention", "epara_cache_attention",
+                     "epara_copy_pages", "epara_page_pool_init", "epara_pages_take", "epara_pages_fork", "epara_pages_free", "epara_pages_compact"):
+            getattr(L, name).restype = i32
         for name in ("epara_batch_rows", "epara_plan_groups", "epara_schedule_tiles", "epara_kernel_classes",
                      "epara_ffn_swiglu_args", "epara_pack_weights", "epara_grouped_forward", "epara_grouped_ffn_swiglu",
                      "epara_request_segments", "epara_copy_segments", "epara_quantize_segments_e4m3", "epara_patch_scales"):
@@ -288,6 +344,88 @@ def epara_attention(h_args, d_args, stream=0):
     h_args = np.ascontiguousarray(h_args, dtype=ATTN_ARGS)
     _check(lib().epara_attention(_ptr(h_args) if len(h_args) else None, int(d_args) or None, len(h_args), int(stream) or None),
            "epara_attention")
+
+
+def epara_add_rmsnorm(h_args, d_args, out_dtype, stream=0):
+    """h_args: RMSNORM_ARGS[G] (host copy, validated); d_args: device address of the same bytes."""
+    h_args = np.ascontiguousarray(h_args, dtype=RMSNORM_ARGS)
+    _check(lib().epara_add_rmsnorm(_ptr(h_args) if len(h_args) else None, int(d_args) or None, len(h_args), int(out_dtype), int(stream) or None),
+           "epara_add_rmsnorm")
+
+
+def epara_plan_cache_append(h_args, table):
+    """h_args: APPEND_ARGS[G]; table: a SequenceTable -> running sums int32[n_seqs + 1]."""
+    h_args = np.ascontiguousarray(h_args, dtype=APPEND_ARGS)
+    first = np.zeros(table.n_seqs + 1, dtype=np.int32)
+    _check(lib().epara_plan_cache_append(_ptr(h_args) if len(h_args) else None, len(h_args), ctypes.addressof(table), _ptr(first)), "epara_plan_cache_append")
+    return first
+
+
+def epara_cache_append(h_args, d_args, table, h_first, d_first, stream=0):
+    h_args = np.ascontiguousarray(h_args, dtype=APPEND_ARGS)
+    _check(lib().epara_cache_append(_ptr(h_args) if len(h_args) else None, int(d_args) or None, len(h_args), ctypes.addressof(table),
+                                    _ptr(h_first), int(d_first) or None, int(stream) or None), "epara_cache_append")
+
+
+def epara_plan_cache_attention(h_args, table, n_compute_units):
+    """-> (running sums int32[2 (n_seqs + 1)], CacheAttnPlan)."""
+    h_args = np.ascontiguousarray(h_args, dtype=CACHE_ATTN_ARGS)
+    first, plan = np.zeros(2 * (table.n_seqs + 1), dtype=np.int32), CacheAttnPlan()
+    _check(lib().epara_plan_cache_attention(_ptr(h_args) if len(h_args) else None, len(h_args), ctypes.addressof(table), int(n_compute_units),
+                                            _ptr(first), ctypes.addressof(plan)), "epara_plan_cache_attention")
+    return first, plan
+
+
+def epara_cache_attention(launch, stream=0):
+    """launch: a CacheAttnLaunch (kept alive, with what it points to, by the caller)."""
+    _check(lib().epara_cache_attention(ctypes.addressof(launch), int(stream) or None), "epara_cache_attention")
+
+
+def epara_copy_pages(h_caches, d_caches, h_moves, d_moves, stream=0):
+    """h_caches: PAGE_COPY[G], h_moves: PAGE_MOVE[n] (host copies, validated); d_*: device addresses of the same bytes."""
+    h_caches, h_moves = np.ascontiguousarray(h_caches, dtype=PAGE_COPY), np.ascontiguousarray(h_moves, dtype=PAGE_MOVE)
+    _check(lib().epara_copy_pages(_ptr(h_caches) if len(h_caches) else None, int(d_caches) or None, len(h_caches),
+                                  _ptr(h_moves) if len(h_moves) else None, int(d_moves) or None, len(h_moves), int(stream) or None), "epara_copy_pages")
+
+
+def epara_page_pool_init(refs, free_pages):
+    """refs, free_pages: int32[n_pages] (kept alive by the caller) -> PagePool."""
+    pool = PagePool()
+    _check(lib().epara_page_pool_init(ctypes.addressof(pool), _ptr(refs), _ptr(free_pages), len(refs)), "epara_page_pool_init")
+    return pool
+
+
+def epara_pages_take(pool, n):
+    """-> int32[n]."""
+    pages = np.zeros(max(int(n), 1), dtype=np.int32)
+    _check(lib().epara_pages_take(ctypes.addressof(pool), int(n), _ptr(pages)), "epara_pages_take")
+    return pages[: int(n)]
+
+
+def epara_pages_fork(pool, pages, tokens):
+    """pages: at least ceil(tokens / 64) of them -> (the child's pages, PAGE_MOVE[0 or 1])."""
+    pages = np.ascontiguousarray(pages, dtype=np.int32)
+    n = -(-int(tokens) // EPARA_CACHE_PAGE)
+    if n > len(pages):
+        raise ValueError("%d tokens lie in %d pages, %d given" % (tokens, n, len(pages)))
+    child, move, n_moves = np.zeros(max(n, 1), dtype=np.int32), np.zeros(1, dtype=PAGE_MOVE), np.zeros(1, dtype=np.int32)
+    _check(lib().epara_pages_fork(ctypes.addressof(pool), _ptr(pages), int(tokens), _ptr(child), _ptr(move), _ptr(n_moves)), "epara_pages_fork")
+    return child[: max(n, 0)], move[: int(n_moves[0])]
+
+
+def epara_pages_free(pool, pages):
+    pages = np.ascontiguousarray(pages, dtype=np.int32)
+    _check(lib().epara_pages_free(ctypes.addressof(pool), _ptr(pages) if len(pages) else None, len(pages)), "epara_pages_free")
+
+
+def epara_pages_compact(pool, table):
+    """table: int32[n], renamed in place -> PAGE_MOVE[n_moves]."""
+    if not (isinstance(table, np.ndarray) and table.dtype == np.int32 and table.flags.c_contiguous):
+        raise ValueError("table is renamed in place: a contiguous int32 array")
+    moves, n_moves = np.zeros(max(pool.n_pages, 1), dtype=PAGE_MOVE), np.zeros(1, dtype=np.int32)
+    _check(lib().epara_pages_compact(ctypes.addressof(pool), _ptr(table) if len(table) else None, len(table), _ptr(moves), len(moves), _ptr(n_moves)),
+           "epara_pages_compact")
+    return moves[: int(n_moves[0])].copy()
 
 
 def epara_dp_group_count(rate_required, rate_of_one_group):

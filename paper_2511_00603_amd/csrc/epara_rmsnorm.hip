@@ -1,0 +1,181 @@
+// libepara: residual + root-mean-square normalisation of decoder blocks, with bf16 or E4M3 output.
+//
+//   s = x + r,  y = s / sqrt(mean(s^2) + eps) * gamma;   8 bits: code = sat(RNE(y / scale))
+//
+// A wave per row: the row is read once and stays in registers; its sum of squares and (8 bits with a scale per row) the
+// maximum of |s gamma| are reduced together, since max |y| = max |s gamma| / sqrt(..).
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "epara.h"
+#include "epara_cast.h"
+
+namespace {
+
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef unsigned int v2u __attribute__((ext_vector_type(2)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+#define EPARA_GLOBAL __attribute__((address_space(1)))
+
+constexpr int NT = 256;
+constexpr int NORM_GRID = 1024;
+
+__device__ __forceinline__ float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f{a, b}), v2bf));
+}
+
+// Group of row `row`: the last one whose first_row is <= row.
+__device__ __forceinline__ int find_group(const epara_rmsnorm_args* __restrict__ args, int G, int row, int first)
+{
+    if (G <= 64) return __builtin_popcountll(__ballot(first <= row)) - 1;
+    int lo = 0, hi = G - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (args[mid].first_row <= row) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
+// CH = 16-byte chunks (8 values) per lane that the widest row of the launch needs.
+template <int CH, bool BITS8>
+__global__ __launch_bounds__(NT) void add_rmsnorm_kernel(const epara_rmsnorm_args* __restrict__ args, int G, int n_rows)
+{
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int first = G <= 64 && lane < G ? args[lane].first_row : 0x7fffffff;
+    for (long next = static_cast<long>(blockIdx.x) * (NT / 64) + wave; next < n_rows; next += gridDim.x * (NT / 64)) {
+        const int global_row = static_cast<int>(next);
+        const epara_rmsnorm_args a = args[__builtin_amdgcn_readfirstlane(find_group(args, G, global_row, first))];
+        const int row = global_row - a.first_row, n_chunks = a.d >> 3;
+        const size_t base = static_cast<size_t>(row) * a.d;
+        const EPARA_GLOBAL char* x = (const EPARA_GLOBAL char*)a.X + base * 2;
+        const EPARA_GLOBAL char* r = a.R ? (const EPARA_GLOBAL char*)a.R + base * 2 : nullptr;
+        const EPARA_GLOBAL float* gamma = (const EPARA_GLOBAL float*)a.gamma;
+        float s[CH][8];
+        float sum = 0.f, top = 0.f;
+        v4i xv[CH], rv[CH];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int chunk = c * 64 + lane;
+            xv[c] = v4i{0, 0, 0, 0};
+            rv[c] = v4i{0, 0, 0, 0};
+            if (chunk < n_chunks) {
+                xv[c] = *reinterpret_cast<const EPARA_GLOBAL v4i*>(x + chunk * 16);
+                if (r) rv[c] = *reinterpret_cast<const EPARA_GLOBAL v4i*>(r + chunk * 16);
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int chunk = c * 64 + lane;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t xu = static_cast<uint32_t>(xv[c][j]), ru = static_cast<uint32_t>(rv[c][j]);
+                s[c][2 * j] = bf16_lo(xu) + bf16_lo(ru);
+                s[c][2 * j + 1] = bf16_hi(xu) + bf16_hi(ru);
+                sum += s[c][2 * j] * s[c][2 * j] + s[c][2 * j + 1] * s[c][2 * j + 1];
+            }
+            if (chunk >= n_chunks) continue;
+            if (a.S) {
+                v4i out;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) out[j] = static_cast<int>(pack_bf16(s[c][2 * j], s[c][2 * j + 1]));
+                *reinterpret_cast<EPARA_GLOBAL v4i*>((EPARA_GLOBAL char*)a.S + base * 2 + chunk * 16) = out;
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const v4f gm = *reinterpret_cast<const EPARA_GLOBAL v4f*>(gamma + chunk * 8 + h * 4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    s[c][4 * h + j] *= gm[j];
+                    if constexpr (BITS8) top = fmaxf(top, fabsf(s[c][4 * h + j]));
+                }
+            }
+        }
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) {
+            sum += __shfl_xor(sum, d);
+            if constexpr (BITS8) top = fmaxf(top, __shfl_xor(top, d));
+        }
+        const float rms = 1.f / sqrtf(sum / static_cast<float>(a.d) + a.eps);
+        float factor = rms;
+        if constexpr (BITS8) {
+            float inv = a.out_inv_scale;
+            if (a.row_scales) {
+                const float scale = top * rms == 0.f ? 1.f : top * rms / 448.f;          // a NaN in the row is a NaN here
+                inv = 1.f / scale;
+                if (lane == 0) ((EPARA_GLOBAL float*)a.row_scales)[row] = scale;
+            }
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int chunk = c * 64 + lane;
+                if (chunk >= n_chunks) continue;
+                float y[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = s[c][j] * factor * inv;
+                const v2u codes = {epara_cast::f32x4_to_e4m3(y[0], y[1], y[2], y[3]), epara_cast::f32x4_to_e4m3(y[4], y[5], y[6], y[7])};
+                *reinterpret_cast<EPARA_GLOBAL v2u*>((EPARA_GLOBAL char*)a.Y + base + chunk * 8) = codes;
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int chunk = c * 64 + lane;
+                if (chunk >= n_chunks) continue;
+                v4i out;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) out[j] = static_cast<int>(pack_bf16(s[c][2 * j] * factor, s[c][2 * j + 1] * factor));
+                *reinterpret_cast<EPARA_GLOBAL v4i*>((EPARA_GLOBAL char*)a.Y + base * 2 + chunk * 16) = out;
+            }
+        }
+    }
+}
+
+template <bool BITS8>
+void enqueue(int per_lane, int grid, hipStream_t s, const epara_rmsnorm_args* d_args, int G, int rows)
+{
+    if (per_lane <= 2)      hipLaunchKernelGGL((add_rmsnorm_kernel<2, BITS8>), dim3(grid), dim3(NT), 0, s, d_args, G, rows);
+    else if (per_lane <= 4) hipLaunchKernelGGL((add_rmsnorm_kernel<4, BITS8>), dim3(grid), dim3(NT), 0, s, d_args, G, rows);
+    else if (per_lane <= 8) hipLaunchKernelGGL((add_rmsnorm_kernel<8, BITS8>), dim3(grid), dim3(NT), 0, s, d_args, G, rows);
+    else                    hipLaunchKernelGGL((add_rmsnorm_kernel<16, BITS8>), dim3(grid), dim3(NT), 0, s, d_args, G, rows);
+}
+
+inline bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+
+}  // namespace
+
+extern "C" int32_t epara_add_rmsnorm(const epara_rmsnorm_args* h_args, const epara_rmsnorm_args* d_args, int32_t G, int32_t out_dtype, void* stream)
+{
+    if (G < 0) return EPARA_ERR_SHAPE;
+    if (out_dtype != EPARA_BF16 && out_dtype != EPARA_FP8_E4M3) return EPARA_ERR_DTYPE;
+    if (G == 0) return EPARA_OK;
+    if (!h_args || !d_args) return EPARA_ERR_NULL;
+    const bool bits8 = out_dtype == EPARA_FP8_E4M3;
+    int64_t rows = 0;
+    int32_t widest = 8;
+    for (int32_t g = 0; g < G; ++g) {
+        const epara_rmsnorm_args& a = h_args[g];
+        if (a.M < 0 || a.d < 8 || a.d > EPARA_NORM_MAX_D || (a.d & 7) || !(a.eps >= 0.f) || !(a.eps < INFINITY)) return EPARA_ERR_SHAPE;
+        if (a.first_row != rows) return EPARA_ERR_SHAPE;
+        if (a.M > 0 && (!a.X || !a.gamma || !a.Y)) return EPARA_ERR_NULL;
+        if (!bits8 && a.row_scales) return EPARA_ERR_SHAPE;
+        if (bits8 && !a.row_scales && (!(a.out_inv_scale > 0.f) || !(a.out_inv_scale < INFINITY))) return EPARA_ERR_SHAPE;
+        if (a.M > 0 && (a.Y == a.S || (bits8 && (a.Y == a.X || a.Y == a.R)))) return EPARA_ERR_SHAPE;
+        if (misaligned(a.X, 16) || misaligned(a.R, 16) || misaligned(a.S, 16) || misaligned(a.Y, 16) || misaligned(a.gamma, 16) || misaligned(a.row_scales, 4)) return EPARA_ERR_ALIGN;
+        rows += a.M;
+        if (a.M > 0 && a.d > widest) widest = a.d;
+        if (rows > INT32_MAX) return EPARA_ERR_SHAPE;
+    }
+    if (rows == 0) return EPARA_OK;
+    const int64_t groups_of_rows = (rows + NT / 64 - 1) / (NT / 64);
+    const int grid = static_cast<int>(groups_of_rows < NORM_GRID ? groups_of_rows : NORM_GRID);
+    const int per_lane = (widest + 511) >> 9;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (bits8) enqueue<true>(per_lane, grid, s, d_args, G, static_cast<int>(rows));
+    else       enqueue<false>(per_lane, grid, s, d_args, G, static_cast<int>(rows));
+    return hipGetLastError() == hipSuccess ? EPARA_OK : EPARA_ERR_HIP;
+}

@@ -293,3 +293,206 @@ class AttnPlan:
 
 def attention(plan, stream=None):
     B.epara_attention(plan.args, plan.d_args.data_ptr(), current_stream_handle() if stream is None else stream)
+
+
+# ---- between the dense layers of a decoder block ------------------------------------------------------
+
+def _want(t, dtype, shape, what, optional=False, strided=False):
+    """The tensor's address, after a look at what the library cannot see: its type, shape and layout.  strided: rows of a wider
+    tensor may be given (elements of a row lie side by side)."""
+    if t is None and optional:
+        return 0
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype:
+        raise ValueError("%s: a %s tensor on the GPU is wanted" % (what, dtype))
+    if t.dim() != len(shape) or any(w is not None and int(w) != int(n) for n, w in zip(t.shape, shape)):
+        raise ValueError("%s: shape %s is wanted, got %s" % (what, tuple(shape), tuple(t.shape)))
+    if t.numel() and not (t.is_contiguous() or (strided and t.stride(-1) == 1)):
+        raise ValueError("%s: rows have to be dense" % what)
+    return t.data_ptr() if t.numel() else 0
+
+
+def _row_stride(t):
+    return int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1])
+
+
+class RmsNormPlan:
+    """Arguments of one epara_add_rmsnorm launch.  groups: per service a dict with the device tensors X [M, d] (bf16), gamma (float32 [d]),
+    Y [M, d] (bf16, or uint8 E4M3 codes; the same for all services), optionally R and S [M, d] and eps; with codes either row_scales (float32 [M],
+    written) or out_scale (the service's static scale)."""
+
+    def __init__(self, groups, device):
+        _require_gpu()
+        self.args = np.zeros(len(groups), dtype=B.RMSNORM_ARGS)
+        kinds = {g["Y"].dtype for g in groups}
+        if len(kinds) > 1 or not kinds <= {torch.bfloat16, torch.uint8}:
+            raise ValueError("Y: bfloat16 or uint8 for all services of a launch")
+        self.out_dtype = B.EPARA_FP8_E4M3 if kinds == {torch.uint8} else B.EPARA_BF16
+        bf, f32, rows = torch.bfloat16, torch.float32, 0
+        for i, g in enumerate(groups):
+            M, d = (int(v) for v in g["X"].shape)
+            out_scale = g.get("out_scale")
+            self.args[i] = (_want(g["X"], bf, (M, d), "X"), _want(g.get("R"), bf, (M, d), "R", True), _want(g["gamma"], f32, (d,), "gamma"),
+                            _want(g.get("S"), bf, (M, d), "S", True), _want(g["Y"], g["Y"].dtype, (M, d), "Y"), _want(g.get("row_scales"), f32, (M,), "row_scales", True),
+                            M, d, float(g.get("eps", 1e-6)), 1.0 / float(out_scale) if out_scale else 0.0, rows, 0)
+            rows += M
+        self.rows = rows
+        self.d_args = _upload(self.args, device)
+        self._keep = [t for g in groups for t in g.values() if isinstance(t, torch.Tensor)]
+
+
+def add_rmsnorm(plan, stream=None):
+    B.epara_add_rmsnorm(plan.args, plan.d_args.data_ptr(), plan.out_dtype, current_stream_handle() if stream is None else stream)
+
+
+class PagedCache:
+    """A service's cache of one layer: codes uint8 [n_pages, kv_heads, 2, 64 * head_dim] (keys, values; E4M3 in the library's
+    order) and scales uint8 [n_pages, kv_heads, 2, 2] (keys, values; blocks of 32 tokens; exponent + 127)."""
+
+    def __init__(self, codes, scales):
+        _want(codes, torch.uint8, (None, None, 2, None), "codes")
+        _want(scales, torch.uint8, (codes.shape[0], codes.shape[1], 2, 2), "scales")
+        self.codes, self.scales = codes, scales
+        self.n_pages, self.kv_heads, self.head_dim = int(codes.shape[0]), int(codes.shape[1]), int(codes.shape[3]) // B.EPARA_CACHE_PAGE
+        if codes.shape[3] != self.head_dim * B.EPARA_CACHE_PAGE:
+            raise ValueError("codes: whole pages of %d tokens" % B.EPARA_CACHE_PAGE)
+
+    @classmethod
+    def empty(cls, n_pages, kv_heads, head_dim, device):
+        return cls(torch.zeros((n_pages, kv_heads, 2, B.EPARA_CACHE_PAGE * head_dim), dtype=torch.uint8, device=device),
+                   torch.zeros((n_pages, kv_heads, 2, 2), dtype=torch.uint8, device=device))
+
+
+class SequenceTable:
+    """The sequences with new tokens of all services, and their pages: uploaded once per step and shared by all layers.  services: per
+    service a list of dicts with first_row, rows, start (position of the first new token) and pages (the sequence's pages in order)."""
+
+    def __init__(self, services, device):
+        _require_gpu()
+        seqs, pages = [], []
+        for g, service in enumerate(services):
+            for s in service:
+                own = [int(p) for p in s["pages"]]
+                seqs.append((g, int(s["first_row"]), int(s["rows"]), int(s["start"]), len(pages), len(own)))
+                pages += own
+        self.G = len(services)
+        self.seqs, self.pages = np.array(seqs, dtype=B.SEQUENCE), np.array(pages, dtype=np.int32)
+        self.d_seqs, self.d_pages = _upload_all([self.seqs, self.pages], device)
+        self.c = B.SequenceTable(self.seqs.ctypes.data, self.d_seqs.data_ptr(), self.pages.ctypes.data, self.d_pages.data_ptr(), len(self.seqs), len(self.pages))
+
+
+class CacheAppendPlan:
+    """Arguments of one epara_cache_append call.  groups: per service of the table a dict with QKV [rows, (heads + 2 kv_heads) head_dim] (bf16), cache
+    (PagedCache), heads, and Q [rows, heads head_dim] (bf16); optionally rotary (float32 [positions, head_dim / 2, 2]: cos, sin), positions
+    (int32 [rows, 3]) and axis_pairs (pairs of each of the three axes).  Without rotary, Q may be left out: the queries stay in QKV."""
+
+    def __init__(self, table, groups, device):
+        _require_gpu()
+        if len(groups) != table.G:
+            raise ValueError("%d services in the table, %d groups" % (table.G, len(groups)))
+        self.table, self.args = table, np.zeros(len(groups), dtype=B.APPEND_ARGS)
+        bf = torch.bfloat16
+        for i, g in enumerate(groups):
+            c, H = g["cache"], int(g["heads"])
+            rows, D = int(g["QKV"].shape[0]), c.head_dim
+            qkv = _want(g["QKV"], bf, (rows, (H + 2 * c.kv_heads) * D), "QKV", strided=True)
+            Q, rotary, positions = g.get("Q"), g.get("rotary"), g.get("positions")
+            pairs = [int(v) for v in g.get("axis_pairs") or (D // 2, 0, 0)]
+            if len(pairs) != 3 or min(pairs) < 0 or sum(pairs) != D // 2:
+                raise ValueError("axis_pairs: three counts that make %d" % (D // 2))
+            self.args[i] = (qkv, _want(Q, bf, (rows, H * D), "Q", True, True), c.codes.data_ptr(), c.scales.data_ptr(),
+                            _want(rotary, torch.float32, (None, D // 2, 2), "rotary", True), _want(positions, torch.int32, (rows, 3), "positions", True),
+                            rows, H, c.kv_heads, D, c.n_pages, _row_stride(g["QKV"]), 0 if Q is None else _row_stride(Q),
+                            0 if rotary is None else int(rotary.shape[0]), pairs[:2])
+        self.first = B.epara_plan_cache_append(self.args, table.c)
+        self.d_args, self.d_first = _upload_all([self.args, self.first], device)
+        self._keep = groups
+
+
+def cache_append(plan, stream=None):
+    B.epara_cache_append(plan.args, plan.d_args.data_ptr(), plan.table.c, plan.first, plan.d_first.data_ptr(),
+                         current_stream_handle() if stream is None else stream)
+
+
+class CacheAttnPlan:
+    """Arguments of one epara_cache_attention call.  groups: per service of the table a dict with Q and O [rows, heads head_dim] (bf16; Q may be the first
+    columns of a QKV projection's output), cache (PagedCache), heads, and optionally scale (1 / sqrt(head_dim)), window and softcap (0: none)."""
+
+    def __init__(self, table, groups, device):
+        _require_gpu()
+        if len(groups) != table.G:
+            raise ValueError("%d services in the table, %d groups" % (table.G, len(groups)))
+        self.table, self.args = table, np.zeros(len(groups), dtype=B.CACHE_ATTN_ARGS)
+        bf = torch.bfloat16
+        for i, g in enumerate(groups):
+            c, H = g["cache"], int(g["heads"])
+            rows, D = int(g["Q"].shape[0]), c.head_dim
+            self.args[i] = (_want(g["Q"], bf, (rows, H * D), "Q", strided=True), _want(g["O"], bf, (rows, H * D), "O", strided=True),
+                            c.codes.data_ptr(), c.scales.data_ptr(), rows, H, c.kv_heads, D, c.n_pages, _row_stride(g["Q"]), _row_stride(g["O"]),
+                            int(g.get("window") or 0), float(g.get("scale") or D ** -0.5), float(g.get("softcap") or 0.0), (0, 0))
+        self.first, self.plan = B.epara_plan_cache_attention(self.args, table.c, n_compute_units(device))
+        self.d_args, self.d_first = _upload_all([self.args, self.first], device)
+        self.d_workspace, at = None, 0
+        if self.plan.workspace_bytes:
+            self.d_workspace = torch.empty(self.plan.workspace_bytes, dtype=torch.uint8, device=device)
+            at = self.d_workspace.data_ptr()
+            counters = 4 * (self.plan.n_items[0] + self.plan.n_items[1])
+            B.epara_workspace_init(at, -(-counters // 256) * 256, current_stream_handle())
+        self.c = B.CacheAttnLaunch(self.args.ctypes.data, self.d_args.data_ptr(), self.first.ctypes.data, self.d_first.data_ptr(), at or None,
+                                   self.plan.workspace_bytes, table.c, self.plan, len(self.args), 0)
+        torch.cuda.synchronize(device)
+        self._keep = groups
+
+
+def cache_attention(plan, stream=None):
+    B.epara_cache_attention(plan.c, current_stream_handle() if stream is None else stream)
+
+
+class PageCopyPlan:
+    """Arguments of one epara_copy_pages call.  groups: per cache a dict with cache (PagedCache) and moves (a list of (from, to), or a PAGE_MOVE array
+    of the library; the layers of a service give the same one)."""
+
+    def __init__(self, groups, device):
+        _require_gpu()
+        self.caches, moves, known, chunks = np.zeros(len(groups), dtype=B.PAGE_COPY), [], {}, 0
+        n = 0
+        for i, g in enumerate(groups):
+            c = g["cache"]
+            if id(g["moves"]) not in known:
+                own = np.array([tuple(m) for m in g["moves"]], dtype=B.PAGE_MOVE)
+                known[id(g["moves"])] = (n, len(own))
+                moves.append(own)
+                n += len(own)
+            first, count = known[id(g["moves"])]
+            self.caches[i] = (c.codes.data_ptr(), c.scales.data_ptr(), c.n_pages, c.kv_heads, c.head_dim, first, count, chunks)
+            chunks += count * c.kv_heads
+        self.moves = np.concatenate(moves) if moves else np.zeros(0, dtype=B.PAGE_MOVE)
+        self.d_caches, self.d_moves = _upload_all([self.caches, self.moves], device)
+        self._keep = groups
+
+
+def copy_pages(plan, stream=None):
+    B.epara_copy_pages(plan.caches, plan.d_caches.data_ptr(), plan.moves, plan.d_moves.data_ptr(), current_stream_handle() if stream is None else stream)
+
+
+class PagePool:
+    """Which page of a cache belongs to whom (host memory only): take, fork, free and compact as in include/epara.h."""
+
+    def __init__(self, n_pages):
+        self.refs, self.free_pages = np.zeros(n_pages, dtype=np.int32), np.zeros(n_pages, dtype=np.int32)
+        self.c = B.epara_page_pool_init(self.refs, self.free_pages)
+
+    @property
+    def n_free(self):
+        return int(self.c.n_free)
+
+    def take(self, n):
+        return B.epara_pages_take(self.c, n)
+
+    def fork(self, pages, tokens):
+        return B.epara_pages_fork(self.c, pages, tokens)
+
+    def free(self, pages):
+        B.epara_pages_free(self.c, pages)
+
+    def compact(self, table):
+        return B.epara_pages_compact(self.c, table)
