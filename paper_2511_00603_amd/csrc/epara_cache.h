@@ -50,7 +50,7 @@ EPARA_BOTH int64_t append_items(const epara_append_args& a, const append_shape& 
 // ---- attention: the rows of a sequence and key head are its tokens x the query heads that share the key head, token by
 // token; a workgroup takes a tile of them against a part of the pages that the tile sees.
 constexpr int FEW_TILE = 16, MANY_TILE = 128;
-constexpr int FEW_MAX_ROWS = 0x7fffffff;
+constexpr int FEW_MAX_ROWS = 32;
 constexpr int SLOT_FLOATS = 128 + 2;                       // per row of a part: the weighted sum of values, maximum, sum of weights
 EPARA_BOTH bool has_few_rows(const epara_cache_attn_args& a, const epara_sequence& s) { return static_cast<int64_t>(s.rows) * (a.heads / a.kv_heads) <= FEW_MAX_ROWS; }
 
