@@ -2,26 +2,25 @@
 //
 //   o = sum_j exp(z_j - m) v_j / sum_j exp(z_j - m),   z_j = scale q . k_j (capped: c tanh(z_j / c)),   m = max_j z_j
 //
-// Keys and values go from memory into the matrix cores as they lie in the cache, E4M3 codes with E8M0 scales: nothing is
-// converted.  A query is the sum of two E4M3 numbers, q = hi + lo / 16 with its own power of two, which holds all 8
-// significant bits of a bf16; so is a weight p = exp(z - m).  Products of 8-bit operands run at twice the rate of bf16
-// ones, so the two products cost what one in bf16 would.  (Weights rounded to bf16 would be 2.7 times coarser.)
+// Both products run on the matrix cores in f16 with fp32 sums.  E4M3 codes widen to f16 exactly, two to an instruction; a query (bf16,
+// 8 significant bits) becomes f16 exactly once its own power of two is taken out, and a weight p = exp(z - m) keeps 11 bits, where bf16
+// would keep 8.  (The 8-bit matrix instructions would take the codes as they are, and a query or weight as the sum of two E4M3 numbers at the
+// same rate; but they hold a sum only to some 2^-12 of its largest term, which is 10^-2 of a weight where a score has terms of 40.)
+// The blocks' scales are powers of two: those of the keys go into the factor between scores and the exponential, those of the values
+// into the exponent of the weights.
 //
-// The matrix cores' scales also carry the running maximum.  The weights of a page are taken relative to the page's own largest score,
-// rounded up to an integer r in units of log 2: p = 2^(z - r), and enter the product with the scale 2^(r - M), where M is the
-// row's reference.  M only has to be near enough for fp32 (MAX_ABOVE), so sums are almost never rescaled, and the weights of a page
-// keep their 8 bits however far they lie under the row's maximum (thousands of keys that share what one strong key leaves).
+// A row's reference M is lazy: weights are 2^(z - M + LIFT) in f16, whose range bears scores ABOVE over M, so sums are
+// rescaled only where a page's largest score exceeds M by more than that (or a block's values have a larger scale than all before).
+// Weights keep their 11 bits down to 2^-23 of M's, so thousands of keys that share what one strong key leaves are held.
 //
 // Both products are written transposed, so that what the first leaves in a lane is what the second wants there:
 //   S^T = K Q^T   A = keys x dims, B = dims x rows;   O^T = V^T P^T   A = dims x tokens, B = tokens x rows
-// For this the cache holds keys and values in the order it does.  In an instruction with a contraction of length C over 64 / N
-// groups of lanes (N rows of B), a lane's first 16 bytes are elements 16 g .. 16 g + 15 of it and its second 16 bytes elements
-// C / 2 + 16 g ..; elements 32 b .. 32 b + 31 take their scale from the lanes of group b.
+// For this the cache holds keys and values in the order it does: a 16-byte chunk is what a lane needs for two instructions.
 //
-//   few rows (a workgroup has a tile of 16): 16x16x128.  Lane (n = lane % 16, q = lane / 16) gets from the four tiles t of S^T of a page the
-//     scores of row n with the keys 16 q + 4 t + 0 .. 3: the 16 tokens of a 16-byte chunk of a dim's values.  O^T takes hi in the first half
-//     and lo in the second against the same values.  Pages go from memory to registers, the four waves take them in turn and meet in the LDS at the end.
-//   many rows (a tile of 128, 32 to a wave): 32x32x64.  Lane (n = lane % 32, h = lane / 32) gets from the two tiles u of S^T of a page the scores of row n
+//   few rows (a workgroup has a tile of 16): 16x16x32.  Lane (n = lane % 16, q = lane / 16) gets from the four tiles t of S^T of a page the
+//     scores of row n with the keys 16 q + 4 t + 0 .. 3: the 16 tokens of a chunk of a dim's values.  Pages go from memory to registers; the four
+//     waves take them in turn and meet in the LDS at the end.
+//   many rows (a tile of 128, 32 to a wave): 32x32x16.  Lane (n = lane % 32, h = lane / 32) gets from the two tiles u of S^T of a page the scores of row n
 //     with the keys 32 u + 16 h + 0 .. 15, again a chunk.  Pages go to the LDS by direct loads, where all four waves read them.
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -39,10 +38,41 @@ namespace {
 constexpr int NT = 256, WAVES = 4;
 constexpr float LOG2E = 1.4426950408889634f;
 
-__device__ __forceinline__ v8i join(v4i a, v4i b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
-__device__ __forceinline__ v4f mfma16(v8i a, v8i b, v4f c, int sa, int sb)
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef unsigned int v2u __attribute__((ext_vector_type(2)));
+
+// Eight E4M3 codes -> eight f16, exactly.
+__device__ __forceinline__ v8h widen(int a, int b)
 {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, sa, 0, sb);
+    const v2h p = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, false), q = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, true);
+    const v2h r = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, false), s = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, true);
+    return v8h{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
+}
+// Eight fp32 -> eight f16, round to nearest even.
+__device__ __forceinline__ v8h narrow(const float* x)
+{
+    const v2h p = __builtin_convertvector((v2f{x[0], x[1]}), v2h), q = __builtin_convertvector((v2f{x[2], x[3]}), v2h);
+    const v2h r = __builtin_convertvector((v2f{x[4], x[5]}), v2h), s = __builtin_convertvector((v2f{x[6], x[7]}), v2h);
+    return v8h{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
+}
+// Eight bf16 times a power of two -> f16.
+__device__ __forceinline__ v8h query8(const v4i& raw, float inv)
+{
+    float x[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        x[2 * j] = bf16_lo(static_cast<uint32_t>(raw[j])) * inv;
+        x[2 * j + 1] = bf16_hi(static_cast<uint32_t>(raw[j])) * inv;
+    }
+    return narrow(x);
+}
+__device__ __forceinline__ float largest8(const v4i& raw)
+{
+    float top = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(fabsf(bf16_lo(static_cast<uint32_t>(raw[j]))), fabsf(bf16_hi(static_cast<uint32_t>(raw[j])))));
+    return top;
 }
 
 // What all kernels know about a workgroup's work.
@@ -94,23 +124,33 @@ __device__ __forceinline__ v2f get2(const float* at)
 
 template <bool V> struct flag { static constexpr bool value = V; };
 constexpr float NOTHING = -1e30f;                          // reference of a row that has seen no key
-constexpr float MAX_ABOVE = 16.f;                          // a page's reference may exceed the row's by that much (sums then grow to 2^(16 + 8) of a value)
-constexpr float LIFT = 8.f;                                // weights are taken as 2^(8 + z - r) <= 2^8: E4M3's upper range; it divides out at the end
+constexpr float ABOVE = 6.f, LIFT = 9.f;                   // a weight is at most 2^(ABOVE + LIFT) = 2^15
 
 struct row_state { float ref, sum; };                      // M, and the sum of the weights relative to it (of this lane's keys)
 
-// The page's reference for a row whose largest score here is `top` (units of log 2; -inf: it sees none of them), and whether the row's own
-// has to be raised.
-__device__ __forceinline__ float page_reference(float top) { return top == -INFINITY ? NOTHING : __builtin_ceilf(top); }
-__device__ __forceinline__ float raise_reference(row_state& s, float ref)
+// What turns sums relative to s.ref into sums relative to the page's largest score `top` (units of log 2; -inf: the row sees none of it), which
+// is s.ref from then on.
+__device__ __forceinline__ float raise_reference(row_state& s, float top)
 {
-    const float to = fmaxf(s.ref, ref), f = __builtin_amdgcn_exp2f(s.ref - to);
+    const float to = top > s.ref ? __builtin_ceilf(top) : s.ref, f = __builtin_amdgcn_exp2f(s.ref - to);
     s.ref = to;
     s.sum *= f;
     return f;
 }
-// Scale byte of the page's weights, hi part.
-__device__ __forceinline__ int weight_scale(const row_state& s, float ref) { return 127 + static_cast<int>(fmaxf(ref - s.ref, -120.f)); }
+
+// The scales of a page and head: keys' and values' exponents of both blocks.  A block behind the last token has whatever the memory holds.
+struct page_scales { float key[2]; int value[2]; };
+__device__ __forceinline__ page_scales scales_of(uint32_t word, bool second_block)
+{
+    page_scales s;
+    s.key[0] = exp2_int(static_cast<int>(word & 0xff) - 127);
+    s.key[1] = exp2_int(static_cast<int>(word >> 8 & 0xff) - 127);
+    s.value[0] = static_cast<int>(word >> 16 & 0xff) - 127;
+    s.value[1] = second_block ? static_cast<int>(word >> 24) - 127 : s.value[0];
+    return s;
+}
+constexpr int NO_SCALE = -1000;                            // the values' reference before any page
+constexpr int LEAST_SHIFT = -60;                           // values under 2^-60 of the largest: their weights are zeros in f16, their sum still is fp32's
 
 __device__ __forceinline__ float capped_score(float z, float in, float out)      // c tanh(z / c) = c (1 - 2 / (1 + e^(2 z / c))), in units of log 2
 {
@@ -139,9 +179,9 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
     const int low_token = w.s.start + w.tile * FEW_TILE / w.group, high_token = w.s.start + (min_of(w.rows, w.tile * FEW_TILE + FEW_TILE) - 1) / w.group;
     const int end = w.s.start + w.s.rows;                  // tokens in the cache
 
-    // ---- the query as two E4M3 numbers: dims 16 q .. and (heads of 128) 64 + 16 q ..
-    v4i qhi[KS], qlo[KS];
-    int q_exp;
+    // ---- the query: dims 16 q .. and (heads of 128) 64 + 16 q .., 8 to an instruction
+    v8h query[KS][2];
+    float q_unit;
     {
         const EPARA_GLOBAL char* src = (const EPARA_GLOBAL char*)a.Q + (static_cast<size_t>(w.s.first_row + token) * a.q_stride + static_cast<size_t>(query_head) * D) * 2;
         v4i raw[KS][2];
@@ -151,27 +191,17 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 raw[s][h] = *reinterpret_cast<const EPARA_GLOBAL v4i*>(src + s * 128 + q * 32 + h * 16);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) amax = fmaxf(amax, fmaxf(fabsf(bf16_lo(raw[s][h][j])), fabsf(bf16_hi(raw[s][h][j]))));
+                amax = fmaxf(amax, largest8(raw[s][h]));
             }
         amax = fmaxf(amax, __shfl_xor(amax, 16));
         amax = fmaxf(amax, __shfl_xor(amax, 32));
-        q_exp = block_exponent(amax);
-        const float inv = exp2_int(-q_exp);
+        const int e = block_exponent(amax);
+        q_unit = exp2_int(e);
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t u = raw[s][j >> 1][(j & 1) * 2], v = raw[s][j >> 1][(j & 1) * 2 + 1];
-                int hi, lo;
-                split_e4m3(bf16_lo(u) * inv, bf16_hi(u) * inv, bf16_lo(v) * inv, bf16_hi(v) * inv, hi, lo);
-                qhi[s][j] = hi;
-                qlo[s][j] = lo;
-            }
+            for (int h = 0; h < 2; ++h) query[s][h] = query8(raw[s][h], exp2_int(-e));
     }
-    // scales of the second operands: heads of 128 take hi and lo in two instructions, heads of 64 in the halves of one
-    const int q_scale_hi = q_exp + 127, q_scale_lo = q_scale_hi - SPLIT_SHIFT, q_scale_both = q < 2 ? q_scale_hi : q_scale_lo;
-    const int p_shift = q < 2 ? 0 : SPLIT_SHIFT;
 
     const size_t head_offset = static_cast<size_t>(w.head) * head_bytes(D);
     const size_t page_bytes = static_cast<size_t>(a.kv_heads) * head_bytes(D);
@@ -189,22 +219,22 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
         for (int d = 0; d < D / 16; ++d) v[d] = *reinterpret_cast<const EPARA_GLOBAL v4i*>(base + PAGE * D + d * 1024);
     };
     auto page_at = [&](int p) { return __builtin_amdgcn_readfirstlane(pages[w.s.first_page + p]); };
-    auto scales_of = [&](int page) { return ((const EPARA_GLOBAL uint32_t*)a.scales)[static_cast<size_t>(page) * a.kv_heads + w.head]; };
+    auto scale_word = [&](int page) { return ((const EPARA_GLOBAL uint32_t*)a.scales)[static_cast<size_t>(page) * a.kv_heads + w.head]; };
 
     row_state state = {NOTHING, 0.f};
+    int v_ref = NO_SCALE;
     v4f o[D / 16];
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) o[d] = v4f{0.f, 0.f, 0.f, 0.f};
-    const float to_log2 = a.scale * LOG2E;
     const bool capped = a.softcap > 0.f;
-    const float cap_in = capped ? 2.f * LOG2E * a.scale / a.softcap : 0.f, cap_out = a.softcap * LOG2E;
+    const float in_unit = (capped ? 2.f * LOG2E * a.scale / a.softcap : a.scale * LOG2E) * q_unit, cap_out = a.softcap * LOG2E;
 
     int p = w.lo + wave;
     const EPARA_GLOBAL char* base = nullptr;
     if (p < w.hi) {
         const int page = page_at(p);
         base = base_of(page);
-        scales = scales_of(page);
+        scales = scale_word(page);
         load_keys(base);
         load_values(base);
     }
@@ -214,31 +244,29 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
         if (more) {
             const int page = page_at(p + WAVES);
             next = base_of(page);
-            scales_next = scales_of(page);
+            scales_next = scale_word(page);
         }
         // ---- scores
+        const page_scales ps = scales_of(scales, p * PAGE + BLOCK < end);
         v4f z[4];
-        const int k_scale = (n < 8 ? scales : scales >> 8) & 0xff;          // row m of a tile: token 16 (m / 4) + .., so block m / 8
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            const v4f zero = {0.f, 0.f, 0.f, 0.f};
-            if constexpr (D == 128) {
-                const v8i key = join(k[t][0], k[t][KS - 1]);
-                z[t] = mfma16(key, join(qhi[0], qhi[KS - 1]), zero, k_scale, q_scale_hi);
-                z[t] = mfma16(key, join(qlo[0], qlo[KS - 1]), z[t], k_scale, q_scale_lo);
-            } else {
-                z[t] = mfma16(join(k[t][0], k[t][0]), join(qhi[0], qlo[0]), zero, k_scale, q_scale_both);
-            }
+            z[t] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    z[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen(k[t][s][2 * h], k[t][s][2 * h + 1]), query[s][h], z[t], 0, 0, 0);
         }
         if (more) load_keys(next);
         const int at = p * PAGE + 16 * q;                  // my keys are at + 4 t + i
-        float unit = to_log2;                              // of a score, to log 2
+        float unit = in_unit * ps.key[q >> 1];             // of a score, to log 2: my keys are of block q / 2
         if (capped) {
-            unit = 1.f;
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) z[t][i] = capped_score(z[t][i], cap_in, cap_out);
+                for (int i = 0; i < 4; ++i) z[t][i] = capped_score(z[t][i], unit, cap_out);
+            unit = 1.f;
         }
         if (p * PAGE + PAGE - 1 > low_token || (a.window > 0 && p * PAGE <= high_token - a.window)) {
 #pragma unroll
@@ -246,42 +274,39 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int key = at + 4 * t + i;
-                    if (key > last_key || key < first_key) z[t][i] = -INFINITY;
+                    z[t][i] = key > last_key || key < first_key ? -INFINITY : z[t][i] * unit;
                 }
+            unit = 1.f;
         }
         // ---- the row's largest score here: mine are 16 keys of the page, the lanes n, n + 16, .. hold the others
         float top = -INFINITY;
 #pragma unroll
         for (int t = 0; t < 4; ++t) top = fmaxf(top, fmaxf(fmaxf(z[t][0], z[t][1]), fmaxf(z[t][2], z[t][3])));
+        top *= unit;
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float ref = page_reference(top * unit);
-        if (__ballot(ref > state.ref + MAX_ABOVE)) {
-            const float f = raise_reference(state, ref);
+        const int v_top = max_of(ps.value[0], ps.value[1]);
+        if (__ballot(top > state.ref + ABOVE || v_top > v_ref)) {
+            const int to = max_of(v_ref, v_top);
+            const float f = raise_reference(state, top) * __builtin_amdgcn_exp2f(static_cast<float>(v_ref - to));
+            v_ref = to;
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) o[d] *= f;
         }
-        const float lift = LIFT - ref;
-        float sum = 0.f;
-        v4i hi, lo;
+        const int v_shift = max_of(ps.value[q >> 1] - v_ref, LEAST_SHIFT);      // <= 0: my values' block against the largest so far
+        const float lift = LIFT - state.ref + static_cast<float>(v_shift);
+        float sum = 0.f, weight[16];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                z[t][i] = __builtin_amdgcn_exp2f(fmaf(z[t][i], unit, lift));
-                sum += z[t][i];
+                weight[4 * t + i] = __builtin_amdgcn_exp2f(fmaf(z[t][i], unit, lift));
+                sum += weight[4 * t + i];
             }
-            int h, r;
-            split_e4m3(z[t][0], z[t][1], z[t][2], z[t][3], h, r);
-            hi[t] = h;
-            lo[t] = r;
-        }
-        state.sum = fmaf(sum, __builtin_amdgcn_exp2f(ref - state.ref), state.sum);
-        const int p_scale = weight_scale(state, ref) - p_shift;
+        state.sum += sum * exp2_int(-v_shift);
+        const v8h w0 = narrow(weight), w1 = narrow(weight + 8);
         // ---- values.  What lies behind the last token may be anything, a NaN too: cleared
-        int v_scale = ((q & 1) ? scales >> 24 : scales >> 16) & 0xff;
         if (p * PAGE + PAGE > end) {
-            if (p * PAGE + BLOCK * (q & 1) >= end) v_scale = 127;
             const int valid = end - at;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -290,15 +315,21 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
                 for (int d = 0; d < D / 16; ++d) v[d][j] &= mask;
             }
         }
-        const v8i weights = join(hi, lo);
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) o[d] = mfma16(join(v[d], v[d]), weights, o[d], v_scale, p_scale);
+        for (int d = 0; d < D / 16; ++d) {
+            o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen(v[d][0], v[d][1]), w0, o[d], 0, 0, 0);
+            o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen(v[d][2], v[d][3]), w1, o[d], 0, 0, 0);
+        }
         if (more) load_values(next);
         base = next;
         scales = scales_next;
     }
     state.sum += __shfl_xor(state.sum, 16);
     state.sum += __shfl_xor(state.sum, 32);
+
+    const float v_unit = v_ref == NO_SCALE ? 0.f : exp2_int(v_ref);
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) o[d] *= v_unit;
 
     // ---- the four waves' sums: thread = (row, D / 16 columns)
 #pragma unroll
@@ -385,18 +416,12 @@ __global__ __launch_bounds__(NT, 2) void attend_few_kernel(const epara_cache_att
 constexpr int RING = 3;                                    // pages in the LDS: one is read, two are on their way
 typedef __attribute__((address_space(3))) char* ldsptr;
 typedef const __attribute__((address_space(4))) uint32_t* constant_words;
-typedef unsigned int v2u __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ v16f mfma32(v8i a, v8i b, v16f c, int sa, int sb)
-{
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, sa, 0, sb);
-}
 __device__ __forceinline__ v4i lds16(ldsptr at) { return *reinterpret_cast<const __attribute__((address_space(3))) v4i*>(at); }
 
 template <int D>
 __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* __restrict__ pages, uint32_t* counters, char* slots, ldsptr ring, int item)
 {
-    constexpr int KS = D / 64, DT = D / 32;                // steps of 64 dims, tiles of 32 dims
+    constexpr int DT = D / 32;                             // tiles of 32 dims
     constexpr int PAGE_BYTES = 2 * PAGE * D, LOADS = PAGE_BYTES / 1024 / WAVES;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, h = lane >> 5;
@@ -409,37 +434,28 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
     const int low_token = w.s.start + min_of(first_row, w.rows - 1) / w.group, high_token = w.s.start + (min_of(w.rows, first_row + 32) - 1) / w.group;
     const int end = w.s.start + w.s.rows;
 
-    // ---- the query: its dims 64 p + 32 h + 16 s ..; hi and lo
-    v8i qhi[KS], qlo[KS];
-    int q_scale;
+    // ---- the query: dims 32 p + 16 h .., 8 to an instruction
+    constexpr int QS = D / 32;
+    v8h query[QS][2];
+    float q_unit;
     {
         const EPARA_GLOBAL char* src = (const EPARA_GLOBAL char*)a.Q + (static_cast<size_t>(w.s.first_row + token) * a.q_stride + static_cast<size_t>(query_head) * D) * 2;
-        v4i raw[KS][4];
+        v4i raw[QS][2];
         float amax = 0.f;
 #pragma unroll
-        for (int p = 0; p < KS; ++p)
+        for (int p = 0; p < QS; ++p)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                raw[p][i] = *reinterpret_cast<const EPARA_GLOBAL v4i*>(src + p * 128 + h * 64 + i * 16);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) amax = fmaxf(amax, fmaxf(fabsf(bf16_lo(raw[p][i][j])), fabsf(bf16_hi(raw[p][i][j]))));
+            for (int i = 0; i < 2; ++i) {
+                raw[p][i] = *reinterpret_cast<const EPARA_GLOBAL v4i*>(src + p * 64 + h * 32 + i * 16);
+                amax = fmaxf(amax, largest8(raw[p][i]));
             }
         amax = fmaxf(amax, __shfl_xor(amax, 32));
         const int e = block_exponent(amax);
-        q_scale = e + 127;
-        const float inv = exp2_int(-e);
+        q_unit = exp2_int(e);
 #pragma unroll
-        for (int p = 0; p < KS; ++p)
+        for (int p = 0; p < QS; ++p)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const uint32_t u = raw[p][i][2 * j], v = raw[p][i][2 * j + 1];
-                    int hi, lo;
-                    split_e4m3(bf16_lo(u) * inv, bf16_hi(u) * inv, bf16_lo(v) * inv, bf16_hi(v) * inv, hi, lo);
-                    qhi[p][2 * i + j] = hi;
-                    qlo[p][2 * i + j] = lo;
-                }
+            for (int i = 0; i < 2; ++i) query[p][i] = query8(raw[p][i], exp2_int(-e));
     }
 
     // ---- pages to the LDS: a wave brings a quarter of each
@@ -458,16 +474,16 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
     };
 
     row_state state = {NOTHING, 0.f};
+    int v_ref = NO_SCALE;
     v16f o[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-    const float to_log2 = a.scale * LOG2E;
     const bool capped = a.softcap > 0.f;
-    const float cap_in = capped ? 2.f * LOG2E * a.scale / a.softcap : 0.f, cap_out = a.softcap * LOG2E;
-    // where my chunks lie in a page: keys, tile u and step p: rows of the tile are the keys 32 u + 16 (row / 4 % 2) + 4 (row / 8) + row % 4
-    const int key_at = ((n >> 3) * (D / 16) + 2 * h) * 256 + (n & 7) * 16, value_at = PAGE * D + ((n >> 4) * 4 + h) * 256 + (n & 15) * 16;
+    const float in_unit = (capped ? 2.f * LOG2E * a.scale / a.softcap : a.scale * LOG2E) * q_unit, cap_out = a.softcap * LOG2E;
+    // where my chunks lie in a page: keys, tile u and dims 32 p + 16 h: rows of the tile are the keys 32 u + 16 (row / 4 % 2) + 4 (row / 8) + row % 4
+    const int key_at = ((n >> 3) * (D / 16) + h) * 256 + (n & 7) * 16, value_at = PAGE * D + ((n >> 4) * 4 + h) * 256 + (n & 15) * 16;
 
     uint32_t sc[2] = {0, 0};                               // scales of the page that is read and of the next one
     if (w.lo < w.hi) sc[0] = fetch(w.lo, 0);
@@ -486,91 +502,94 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
         if (!live || p * PAGE > high_token || (a.window > 0 && p * PAGE + PAGE <= low_token - a.window + 1)) continue;
 
         // ---- scores
+        const page_scales ps = scales_of(now, p * PAGE + BLOCK < end);
         v16f z[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int k_scale = now >> (8 * u) & 0xff;
 #pragma unroll
             for (int i = 0; i < 16; ++i) z[u][i] = 0.f;
 #pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                const v8i key = join(lds16(here + key_at + u * 128 + s * 1024), lds16(here + key_at + u * 128 + s * 1024 + 256));
-                z[u] = mfma32(key, qhi[s], z[u], k_scale, q_scale);
-                z[u] = mfma32(key, qlo[s], z[u], k_scale, q_scale - SPLIT_SHIFT);
+            for (int s = 0; s < QS; ++s) {
+                const v4i key = lds16(here + key_at + u * 128 + s * 512);
+                z[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen(key[0], key[1]), query[s][0], z[u], 0, 0, 0);
+                z[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen(key[2], key[3]), query[s][1], z[u], 0, 0, 0);
             }
         }
-        float unit = to_log2;
+        float unit[2] = {in_unit * ps.key[0], in_unit * ps.key[1]};          // of a score, to log 2
         if (capped) {
-            unit = 1.f;
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < 2; ++u) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) z[u][i] = capped_score(z[u][i], cap_in, cap_out);
+                for (int i = 0; i < 16; ++i) z[u][i] = capped_score(z[u][i], unit[u], cap_out);
+                unit[u] = 1.f;
+            }
         }
         if (p * PAGE + PAGE - 1 > low_token || (a.window > 0 && p * PAGE <= high_token - a.window)) {
             const int last = last_key - p * PAGE - 16 * h, from = first_key - p * PAGE - 16 * h;
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (32 * u + i > last || 32 * u + i < from) z[u][i] = -INFINITY;
+                for (int i = 0; i < 16; ++i) z[u][i] = 32 * u + i > last || 32 * u + i < from ? -INFINITY : z[u][i] * unit[u];
+            unit[0] = unit[1] = 1.f;
         }
         // ---- weights
-        float top = fmaxf(z[0][0], z[1][0]);
+        float top_of[2];
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, fmaxf(z[0][i], z[1][i]));
+        for (int u = 0; u < 2; ++u) {
+            top_of[u] = fmaxf(z[u][0], z[u][1]);
+#pragma unroll
+            for (int i = 2; i < 16; i += 2) top_of[u] = fmaxf(top_of[u], fmaxf(z[u][i], z[u][i + 1]));
+        }
+        float top = fmaxf(top_of[0] * unit[0], top_of[1] * unit[1]);
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float ref = page_reference(top * unit);
-        if (__ballot(ref > state.ref + MAX_ABOVE)) {
-            const float f = raise_reference(state, ref);
+        const int v_top = max_of(ps.value[0], ps.value[1]);
+        if (__ballot(top > state.ref + ABOVE || v_top > v_ref)) {
+            const int to = max_of(v_ref, v_top);
+            const float f = raise_reference(state, top) * __builtin_amdgcn_exp2f(static_cast<float>(v_ref - to));
+            v_ref = to;
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[d][i] *= f;
         }
-        const float lift = LIFT - ref;
-        float sum[2] = {0.f, 0.f};
-        v8i hi, lo;
+        v8h weights[2][2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < 2; ++u) {
+            const int v_shift = max_of(ps.value[u] - v_ref, LEAST_SHIFT);       // <= 0
+            const float lift = LIFT - state.ref + static_cast<float>(v_shift);
+            float sum = 0.f, x[16];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float x[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    x[i] = __builtin_amdgcn_exp2f(fmaf(z[u][4 * j + i], unit, lift));
-                    sum[u] += x[i];
-                }
-                int a4, b4;
-                split_e4m3(x[0], x[1], x[2], x[3], a4, b4);
-                hi[4 * u + j] = a4;
-                lo[4 * u + j] = b4;
+            for (int i = 0; i < 16; ++i) {
+                x[i] = __builtin_amdgcn_exp2f(fmaf(z[u][i], unit[u], lift));
+                sum += x[i];
             }
-        state.sum = fmaf(sum[0] + sum[1], __builtin_amdgcn_exp2f(ref - state.ref), state.sum);
-        const int p_scale = weight_scale(state, ref);
+            state.sum += sum * exp2_int(-v_shift);
+            weights[u][0] = narrow(x);
+            weights[u][1] = narrow(x + 8);
+        }
         // ---- values.  What lies behind the last token may be anything, a NaN too: cleared
-        int v_scale = now >> (16 + 8 * h) & 0xff;
-        const bool ragged = p * PAGE + PAGE > end;
-        if (ragged && p * PAGE + BLOCK * h >= end) v_scale = 127;
         auto add_values = [&](auto clear_tag) {
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                v4i v0 = lds16(here + value_at + d * 2048), v1 = lds16(here + value_at + d * 2048 + 512);
-                if constexpr (decltype(clear_tag)::value) {
-                    const int valid = end - p * PAGE - 16 * h;
+            for (int d = 0; d < DT; ++d)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        v0[j] &= low_bytes(valid - 4 * j);
-                        v1[j] &= low_bytes(valid - BLOCK - 4 * j);
+                for (int u = 0; u < 2; ++u) {
+                    v4i value = lds16(here + value_at + d * 2048 + u * 512);
+                    if constexpr (decltype(clear_tag)::value) {
+                        const int valid = end - p * PAGE - BLOCK * u - 16 * h;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) value[j] &= low_bytes(valid - 4 * j);
                     }
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen(value[0], value[1]), weights[u][0], o[d], 0, 0, 0);
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen(value[2], value[3]), weights[u][1], o[d], 0, 0, 0);
                 }
-                const v8i value = join(v0, v1);
-                o[d] = mfma32(value, hi, o[d], v_scale, p_scale);
-                o[d] = mfma32(value, lo, o[d], v_scale, p_scale - SPLIT_SHIFT);
-            }
         };
-        if (ragged) add_values(flag<true>{}); else add_values(flag<false>{});
+        if (p * PAGE + PAGE > end) add_values(flag<true>{}); else add_values(flag<false>{});
     }
+    const float v_unit = v_ref == NO_SCALE ? 0.f : exp2_int(v_ref);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] *= v_unit;
     state.sum += __shfl_xor(state.sum, 32);
 
     if (w.parts > 1) {

@@ -1,5 +1,5 @@
-// Device helpers of the kernels on the paged cache: vector types, E4M3 conversions, splitting of a number into two E4M3
-// numbers, and the search for the sequence of a work item.
+// Device helpers of the kernels on the paged cache: vector types, E4M3 conversions, a block's exponent,
+// and the search for the sequence of a work item.
 #ifndef EPARA_CACHE_DEVICE_H
 #define EPARA_CACHE_DEVICE_H
 
@@ -12,7 +12,6 @@
 namespace {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
-typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v2f __attribute__((ext_vector_type(2)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
@@ -33,16 +32,6 @@ __device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d)
     return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true));
 }
 __device__ __forceinline__ float clamp448(float x) { return __builtin_amdgcn_fmed3f(x, -448.f, 448.f); }
-
-// x = hi + lo / 16 with hi and lo in E4M3: hi keeps the upper 4 of x's significant bits, the rest has at most 4 more of a
-// bf16's 8, so a bf16 between 2^-6 and 448 is represented exactly (smaller ones to 2^-14), and any x to 2^-8 of its value.
-__device__ __forceinline__ void split_e4m3(float a, float b, float c, float d, int& hi, int& lo)
-{
-    hi = static_cast<int>(to_e4m3(a, b, c, d));
-    const v2f p = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), q = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
-    lo = static_cast<int>(to_e4m3((a - p[0]) * 16.f, (b - p[1]) * 16.f, (c - q[0]) * 16.f, (d - q[1]) * 16.f));
-}
-constexpr int SPLIT_SHIFT = 4;                            // lo's exponent under hi's
 
 // The smallest e in [-96, 120] with amax <= 448 * 2^e; 448 = 1.75 * 2^8.
 __device__ __forceinline__ int block_exponent(float amax)

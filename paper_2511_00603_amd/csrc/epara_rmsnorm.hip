@@ -163,7 +163,7 @@ extern "C" int32_t epara_add_rmsnorm(const epara_rmsnorm_args* h_args, const epa
         if (a.first_row != rows) return EPARA_ERR_SHAPE;
         if (a.M > 0 && (!a.X || !a.gamma || !a.Y)) return EPARA_ERR_NULL;
         if (!bits8 && a.row_scales) return EPARA_ERR_SHAPE;
-        if (bits8 && !a.row_scales && (!(a.out_inv_scale > 0.f) || !(a.out_inv_scale < INFINITY))) return EPARA_ERR_SHAPE;
+        if (bits8 && a.M > 0 && !a.row_scales && (!(a.out_inv_scale > 0.f) || !(a.out_inv_scale < INFINITY))) return EPARA_ERR_SHAPE;
         if (a.M > 0 && (a.Y == a.S || (bits8 && (a.Y == a.X || a.Y == a.R)))) return EPARA_ERR_SHAPE;
         if (misaligned(a.X, 16) || misaligned(a.R, 16) || misaligned(a.S, 16) || misaligned(a.Y, 16) || misaligned(a.gamma, 16) || misaligned(a.row_scales, 4)) return EPARA_ERR_ALIGN;
         rows += a.M;
