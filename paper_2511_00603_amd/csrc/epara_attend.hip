@@ -111,7 +111,7 @@ __device__ __forceinline__ work_item find_work(const epara_cache_attn_args* __re
     return w;
 }
 
-// 16 bytes that another die has written or will read in this kernel: through to memory, past the dies' own caches.
+// 8 bytes that a workgroup on another die has written or will read in this kernel: past the dies' own caches.
 __device__ __forceinline__ void put2(float* at, float a, float b)
 {
     __hip_atomic_store(reinterpret_cast<unsigned long long*>(at), (static_cast<unsigned long long>(__float_as_uint(b)) << 32) | __float_as_uint(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -159,13 +159,98 @@ __device__ __forceinline__ float capped_score(float z, float in, float out)     
 
 template <int D>
 struct few_lds {
-    float o[WAVES][FEW_TILE][D + 4];
+    union {
+        float o[WAVES][FEW_TILE][D + 4];                   // a part: the waves' sums
+        v4f joined[WAVES][FEW_TILE * D / 4];               // joining the parts: the waves' sums again
+    };
     float m[WAVES][FEW_TILE], l[WAVES][FEW_TILE];
+    float weight[MAX_PARTS][FEW_TILE];                     // of a part's sums in the result
     uint32_t last;
 };
 
+// 16 bytes that a workgroup on another die has written or will read in this kernel: past the dies' own caches (16: device scope).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t slot_of(char* slots, size_t item, int bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(slots + item * bytes, 0, bytes, 0x00020000);
+}
+__device__ __forceinline__ void put4(__amdgpu_buffer_rsrc_t slot, int at, v4f x) { __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4i, x), slot, at, 0, 16); }
+__device__ __forceinline__ v4f get4(__amdgpu_buffer_rsrc_t slot, int at) { return __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(slot, at, 0, 16)); }
+
+// Four consecutive columns of an output row of a tile of `size` rows.
+__device__ __forceinline__ void store_out4(const work_item& w, int row, int col, v4f x)
+{
+    const int token = row / w.group, head = w.head * w.group + row - token * w.group;
+    EPARA_GLOBAL char* dst = (EPARA_GLOBAL char*)w.a.O + (static_cast<size_t>(w.s.first_row + token) * w.a.o_stride + static_cast<size_t>(head) * w.a.head_dim + col) * 2;
+    *reinterpret_cast<EPARA_GLOBAL v2u*>(dst) = v2u{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+}
+
+// A slot of few rows: 16 rows of D sums, then 16 pairs (reference, sum of weights).
+constexpr int FEW_SLOT = FEW_TILE * SLOT_FLOATS * 4;
+
+// All parts of a tile are in their slots: their weighted sum, in the order of the parts inside a wave and of the waves, so the same bits every time.
 template <int D>
-__device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __restrict__ pages, uint32_t* counters, float* slots, char* lds_bytes, int item)
+__device__ __forceinline__ void join_few(const work_item& w, char* slots, few_lds<D>& lds, int wave, int lane)
+{
+    const int tid = wave * 64 + lane, rows = min_of(FEW_TILE, w.rows - w.tile * FEW_TILE);
+    {   // thread = (row, one of 16): weights of the parts.  A row that sees no key: zeros
+        const int r = tid >> 4, j = tid & 15;
+        float ref[MAX_PARTS / 16], sum[MAX_PARTS / 16], top = NOTHING;
+#pragma unroll
+        for (int i = 0; i < MAX_PARTS / 16; ++i) {
+            ref[i] = NOTHING;
+            sum[i] = 0.f;
+            if (j + 16 * i < w.parts && r < rows) {
+                const v2f ml = get2(reinterpret_cast<const float*>(slots + (w.first_item + static_cast<size_t>(j + 16 * i) * w.stride) * FEW_SLOT) + FEW_TILE * D + 2 * r);
+                ref[i] = ml[0];
+                sum[i] = ml[1];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < MAX_PARTS / 16; ++i) top = fmaxf(top, ref[i]);
+#pragma unroll
+        for (int d = 8; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+        float total = 0.f;
+#pragma unroll
+        for (int i = 0; i < MAX_PARTS / 16; ++i) {
+            ref[i] = __builtin_amdgcn_exp2f(ref[i] - top);
+            total += sum[i] * ref[i];
+        }
+#pragma unroll
+        for (int d = 8; d >= 1; d >>= 1) total += __shfl_xor(total, d);
+        const float inv = top == NOTHING ? 0.f : 1.f / total;
+#pragma unroll
+        for (int i = 0; i < MAX_PARTS / 16; ++i)
+            if (j + 16 * i < w.parts) lds.weight[j + 16 * i][r] = ref[i] * inv;
+    }
+    __syncthreads();
+    constexpr int STEPS = FEW_TILE * D / 256;              // 16-byte pieces of a slot per lane
+    const int pieces = rows * D / 4;
+    v4f acc[STEPS];
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k) acc[k] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = wave; i < w.parts; i += WAVES) {
+        const __amdgpu_buffer_rsrc_t slot = slot_of(slots, w.first_item + static_cast<size_t>(i) * w.stride, FEW_SLOT);
+#pragma unroll
+        for (int k = 0; k < STEPS; ++k) {
+            if (k * 64 >= pieces) break;
+            const int e = lane + 64 * k;                   // a piece past the rows reads what the slot holds, and is not stored
+            acc[k] += get4(slot, e * 16) * lds.weight[i][e / (D / 4)];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k) lds.joined[wave][lane + 64 * k] = acc[k];
+    __syncthreads();
+    for (int e = tid; e < pieces; e += NT) {
+        v4f x = lds.joined[0][e];
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i) x += lds.joined[i][e];
+        store_out4(w, w.tile * FEW_TILE + e / (D / 4), e % (D / 4) * 4, x);
+    }
+}
+
+template <int D>
+__device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __restrict__ pages, uint32_t* counters, char* slots, char* lds_bytes, int item)
 {
     few_lds<D>& lds = *reinterpret_cast<few_lds<D>*>(lds_bytes);
     constexpr int KS = D / 64;                             // 16-byte pieces of a key that a lane holds
@@ -212,11 +297,11 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int s = 0; s < KS; ++s) k[t][s] = *reinterpret_cast<const EPARA_GLOBAL v4i*>(base + (t * KS + s) * 1024);
+            for (int s = 0; s < KS; ++s) k[t][s] = __builtin_nontemporal_load(reinterpret_cast<const EPARA_GLOBAL v4i*>(base + (t * KS + s) * 1024));
     };
     auto load_values = [&](const EPARA_GLOBAL char* base) {
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) v[d] = *reinterpret_cast<const EPARA_GLOBAL v4i*>(base + PAGE * D + d * 1024);
+        for (int d = 0; d < D / 16; ++d) v[d] = __builtin_nontemporal_load(reinterpret_cast<const EPARA_GLOBAL v4i*>(base + PAGE * D + d * 1024));
     };
     auto page_at = [&](int p) { return __builtin_amdgcn_readfirstlane(pages[w.s.first_page + p]); };
     auto scale_word = [&](int page) { return ((const EPARA_GLOBAL uint32_t*)a.scales)[static_cast<size_t>(page) * a.kv_heads + w.head]; };
@@ -260,7 +345,7 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
         }
         if (more) load_keys(next);
         const int at = p * PAGE + 16 * q;                  // my keys are at + 4 t + i
-        float unit = in_unit * ps.key[q >> 1];             // of a score, to log 2: my keys are of block q / 2
+        float unit = in_unit * (q < 2 ? ps.key[0] : ps.key[1]);             // of a score, to log 2: my keys are of block q / 2
         if (capped) {
 #pragma unroll
             for (int t = 0; t < 4; ++t)
@@ -293,7 +378,7 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) o[d] *= f;
         }
-        const int v_shift = max_of(ps.value[q >> 1] - v_ref, LEAST_SHIFT);      // <= 0: my values' block against the largest so far
+        const int v_shift = max_of((q < 2 ? ps.value[0] : ps.value[1]) - v_ref, LEAST_SHIFT);      // <= 0: my values' block against the largest so far
         const float lift = LIFT - state.ref + static_cast<float>(v_shift);
         float sum = 0.f, weight[16];
 #pragma unroll
@@ -354,12 +439,12 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
         for (int j = 0; j < COLS; ++j) oo[j] += weight * lds.o[i][r][c + j];
     }
     const int out_row = w.tile * FEW_TILE + r;
-    if (w.parts > 1) {                                     // the part's sums go to its slot; who ends last adds up all of them, in order
-        float* slot = slots + static_cast<size_t>(item) * FEW_TILE * SLOT_FLOATS + r * SLOT_FLOATS;
+    if (w.parts > 1) {                                     // the part's sums go to its slot; who ends last adds up all of them
+        const __amdgpu_buffer_rsrc_t slot = slot_of(slots, item, FEW_SLOT);
         if (out_row < w.rows) {
 #pragma unroll
-            for (int j = 0; j < COLS; j += 2) put2(slot + c + j, oo[j], oo[j + 1]);
-            if (c == 0) put2(slot + 128, mm, ll);
+            for (int j = 0; j < COLS; j += 4) put4(slot, (r * D + c + j) * 4, v4f{oo[j], oo[j + 1], oo[j + 2], oo[j + 3]});
+            if (c == 0) put2(reinterpret_cast<float*>(slots + static_cast<size_t>(item) * FEW_SLOT) + FEW_TILE * D + 2 * r, mm, ll);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
@@ -367,41 +452,18 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
         __syncthreads();
         if (!lds.last) return;
         if (tid == 0) __hip_atomic_store(counters + w.first_item, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (out_row >= w.rows) return;
-        mm = NOTHING;
-        ll = 0.f;
-#pragma unroll
-        for (int j = 0; j < COLS; ++j) oo[j] = 0.f;
-        const float* from = slots + static_cast<size_t>(w.first_item) * FEW_TILE * SLOT_FLOATS + r * SLOT_FLOATS;
-        for (int i = 0; i < w.parts; ++i, from += static_cast<size_t>(w.stride) * FEW_TILE * SLOT_FLOATS) {
-            const v2f ml = get2(from + 128);
-            const float both = fmaxf(mm, ml[0]), keep = __builtin_amdgcn_exp2f(mm - both), add = __builtin_amdgcn_exp2f(ml[0] - both);
-            mm = both;
-            ll = ll * keep + ml[1] * add;
-#pragma unroll
-            for (int j = 0; j < COLS; j += 2) {
-                const v2f x = get2(from + c + j);
-                oo[j] = oo[j] * keep + x[0] * add;
-                oo[j + 1] = oo[j + 1] * keep + x[1] * add;
-            }
-        }
+        join_few<D>(w, slots, lds, wave, lane);
+        return;
     }
     if (out_row >= w.rows) return;
-    const float inv = mm == NOTHING ? 0.f : 1.f / ll;    // a row that sees no key: zeros
-    const int out_token = out_row / w.group, out_head = w.head * w.group + out_row - out_token * w.group;
-    EPARA_GLOBAL char* dst = (EPARA_GLOBAL char*)a.O + (static_cast<size_t>(w.s.first_row + out_token) * a.o_stride + static_cast<size_t>(out_head) * D + c) * 2;
-    if constexpr (D == 128) {
-        *reinterpret_cast<EPARA_GLOBAL v4i*>(dst) = v4i{static_cast<int>(pack_bf16(oo[0] * inv, oo[1] * inv)), static_cast<int>(pack_bf16(oo[2] * inv, oo[3] * inv)),
-                                                        static_cast<int>(pack_bf16(oo[COLS - 4] * inv, oo[COLS - 3] * inv)), static_cast<int>(pack_bf16(oo[COLS - 2] * inv, oo[COLS - 1] * inv))};
-    } else {
-        typedef unsigned int v2u __attribute__((ext_vector_type(2)));
-        *reinterpret_cast<EPARA_GLOBAL v2u*>(dst) = v2u{pack_bf16(oo[0] * inv, oo[1] * inv), pack_bf16(oo[2] * inv, oo[3] * inv)};
-    }
+    const float inv = mm == NOTHING ? 0.f : 1.f / ll;      // a row that sees no key: zeros
+#pragma unroll
+    for (int j = 0; j < COLS; j += 4) store_out4(w, out_row, c + j, v4f{oo[j], oo[j + 1], oo[j + 2], oo[j + 3]} * inv);
 }
 
 __global__ __launch_bounds__(NT, 2) void attend_few_kernel(const epara_cache_attn_args* __restrict__ args, const epara_sequence* __restrict__ seqs,
                                                           const int32_t* __restrict__ pages, const int32_t* __restrict__ first, int n_seqs, int part_pages,
-                                                          uint32_t* counters, float* slots)
+                                                          uint32_t* counters, char* slots)
 {
     __shared__ __attribute__((aligned(16))) char lds[sizeof(few_lds<128>)];
     const int item = blockIdx.x;
@@ -693,6 +755,6 @@ extern "C" int32_t epara_cache_attention(const epara_cache_attn_launch* launch, 
                            l.d_first + l.table.n_seqs + 1, l.table.n_seqs, l.plan.part_pages[1], counters + l.plan.n_items[0], many_slots);
     if (l.plan.n_items[0] > 0)
         hipLaunchKernelGGL(attend_few_kernel, dim3(static_cast<unsigned>(l.plan.n_items[0])), dim3(NT), 0, s, l.d_args, l.table.d_seqs, l.table.d_pages, l.d_first,
-                           l.table.n_seqs, l.plan.part_pages[0], counters, reinterpret_cast<float*>(slots));
+                           l.table.n_seqs, l.plan.part_pages[0], counters, slots);
     return hipGetLastError() == hipSuccess ? EPARA_OK : EPARA_ERR_HIP;
 }

@@ -51,6 +51,7 @@ EPARA_BOTH int64_t append_items(const epara_append_args& a, const append_shape& 
 // token; a workgroup takes a tile of them against a part of the pages that the tile sees.
 constexpr int FEW_TILE = 16, MANY_TILE = 128;
 constexpr int FEW_MAX_ROWS = 32;
+constexpr int MAX_PARTS = 128;                             // of a tile's pages
 constexpr int SLOT_FLOATS = 128 + 2;                       // per row of a part: the weighted sum of values, maximum, sum of weights
 EPARA_BOTH bool has_few_rows(const epara_cache_attn_args& a, const epara_sequence& s) { return static_cast<int64_t>(s.rows) * (a.heads / a.kv_heads) <= FEW_MAX_ROWS; }
 

@@ -169,6 +169,7 @@ int32_t count_attn(const epara_cache_attn_args* args, const epara_sequence_table
             const page_range r = pages_of_tile(a, s, w.few, tile);
             parts = std::max(parts, ceil_div(r.hi - r.lo, part_pages[k]));
         }
+        if (parts > MAX_PARTS) return EPARA_ERR_SHAPE;
         if (parts > 1) cut[k] = true;
         items[k] += parts * w.tiles * a.kv_heads;
         if (items[k] > INT32_MAX / 256) return EPARA_ERR_CAPACITY;
@@ -266,20 +267,20 @@ int32_t epara_plan_cache_attention(const epara_cache_attn_args* h_args, int32_t 
     if (const int32_t rc = check_attn(h_args, G, table)) return rc;
     if (!first || !plan) return EPARA_ERR_NULL;
     if (n_compute_units < 1 || n_compute_units > 65536) return EPARA_ERR_SHAPE;
-    int64_t work[2] = {0, 0}, tiles[2] = {0, 0};
+    int64_t work[2] = {0, 0}, longest[2] = {0, 0};
     for (int32_t i = 0; i < table->n_seqs; ++i) {
         const epara_sequence& s = table->h_seqs[i];
         const epara_cache_attn_args& a = h_args[s.service];
         if (s.rows == 0) continue;
         const seq_tiles w = tiles_of(a, s);
         const int k = w.few ? 0 : 1;
-        tiles[k] += static_cast<int64_t>(w.tiles) * a.kv_heads;
         for (int tile = 0; tile < w.tiles; ++tile) {
             const page_range r = pages_of_tile(a, s, w.few, tile);
             work[k] += static_cast<int64_t>(r.hi - r.lo) * a.kv_heads;
+            longest[k] = std::max<int64_t>(longest[k], r.hi - r.lo);
         }
     }
-    epara_attn_part_pages(work, tiles, n_compute_units, plan->part_pages);
+    epara_attn_part_pages(work, longest, n_compute_units, plan->part_pages);
     bool cut[2];
     if (const int32_t rc = count_attn(h_args, table, plan->part_pages, first, nullptr, plan->n_items, cut)) return rc;
     plan->workspace_bytes = attn_workspace(plan->n_items, cut);
