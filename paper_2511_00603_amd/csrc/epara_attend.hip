@@ -21,7 +21,7 @@
 //     scores of row n with the keys 16 q + 4 t + 0 .. 3: the 16 tokens of a chunk of a dim's values.  Pages go from memory to registers; the four
 //     waves take them in turn and meet in the LDS at the end.
 //   many rows (a tile of 128, 32 to a wave): 32x32x16.  Lane (n = lane % 32, h = lane / 32) gets from the two tiles u of S^T of a page the scores of row n
-//     with the keys 32 u + 16 h + 0 .. 15, again a chunk.  Pages go to the LDS by direct loads, where all four waves read them.
+//     with the keys 32 u + 16 h + 0 .. 15, again a chunk.  Pages go through the registers, where they are widened once for all four waves, to the LDS.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -151,6 +151,14 @@ __device__ __forceinline__ page_scales scales_of(uint32_t word, bool second_bloc
 }
 constexpr int NO_SCALE = -1000;                            // the values' reference before any page
 constexpr int LEAST_SHIFT = -60;                           // values under 2^-60 of the largest: their weights are zeros in f16, their sum still is fp32's
+
+// The largest of three; a NaN does not count.  (fmaxf first makes sure that its operands are no signalling NaNs: an instruction each.)
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
 
 __device__ __forceinline__ float capped_score(float z, float in, float out)      // c tanh(z / c) = c (1 - 2 / (1 + e^(2 z / c))), in units of log 2
 {
@@ -475,16 +483,16 @@ __global__ __launch_bounds__(NT, 2) void attend_few_kernel(const epara_cache_att
 
 // ---- many rows -------------------------------------------------------------------------------------------------
 
-constexpr int RING = 3;                                    // pages in the LDS: one is read, two are on their way
 typedef __attribute__((address_space(3))) char* ldsptr;
 typedef const __attribute__((address_space(4))) uint32_t* constant_words;
-__device__ __forceinline__ v4i lds16(ldsptr at) { return *reinterpret_cast<const __attribute__((address_space(3))) v4i*>(at); }
+__device__ __forceinline__ v8h lds8h(ldsptr at) { return *reinterpret_cast<const __attribute__((address_space(3))) v8h*>(at); }
+__device__ __forceinline__ void lds_put(ldsptr at, v8h x) { *reinterpret_cast<__attribute__((address_space(3))) v8h*>(at) = x; }
 
 template <int D>
 __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* __restrict__ pages, uint32_t* counters, char* slots, ldsptr ring, int item)
 {
     constexpr int DT = D / 32;                             // tiles of 32 dims
-    constexpr int PAGE_BYTES = 2 * PAGE * D, LOADS = PAGE_BYTES / 1024 / WAVES;
+    constexpr int PAGE_BYTES = 2 * PAGE * D, LOADS = PAGE_BYTES / 1024 / WAVES, VALUES = PAGE * D * 2;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, h = lane >> 5;
     const epara_cache_attn_args& a = w.a;
@@ -520,19 +528,43 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
             for (int i = 0; i < 2; ++i) query[p][i] = query8(raw[p][i], exp2_int(-e));
     }
 
-    // ---- pages to the LDS: a wave brings a quarter of each
+    // ---- pages to the LDS, widened on the way: a wave brings a quarter of each, waves 0 and 1 the keys.  A page in the LDS is in f16, in pieces of
+    // 1 KiB of which lane l reads 16 bytes at 16 l: keys (tile u, dims 32 s + 16 h + 8 j ..), then values (dims 32 d .., tile u, tokens 16 h + 8 j ..)
     const constant_words table = (constant_words)(pages + w.s.first_page);
     const constant_words scales = (constant_words)a.scales;
     const size_t page_bytes = static_cast<size_t>(a.kv_heads) * PAGE_BYTES;
-    auto fetch = [&](int p, int slot) -> uint32_t {        // returns the page's scales
+    const bool brings_values = wave >= 2;
+    const int piece = (wave & 1) * LOADS;                  // of its half of the page
+    const int put_at = brings_values ? VALUES + (lane >> 5) * 2048 + ((lane >> 4) & 1) * 512 + (lane & 15) * 16
+                                     : ((lane >> 3) & 1) * (D * 64) + (lane >> 5) * 2048 + ((lane >> 4) & 1) * 512 + (lane & 7) * 16;
+    v4i raw[LOADS];
+    auto fetch = [&](int p) -> uint32_t {                  // returns the page's scales
         const uint32_t page = table[p];
-        const char* base = static_cast<const char*>(a.codes) + page * page_bytes + static_cast<size_t>(w.head) * PAGE_BYTES;
-        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, PAGE_BYTES, 0x00020000);
+        const EPARA_GLOBAL char* base = (const EPARA_GLOBAL char*)a.codes + page * page_bytes + static_cast<size_t>(w.head) * PAGE_BYTES + wave * LOADS * 1024 + lane * 16;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) raw[i] = *reinterpret_cast<const EPARA_GLOBAL v4i*>(base + i * 1024);
+        return scales[static_cast<size_t>(page) * a.kv_heads + w.head];
+    };
+    auto clear_behind = [&](int p) {                       // values behind the last token may be anything, a NaN too
+        if (!brings_values || p * PAGE + PAGE <= end) return;
+        const int valid = end - p * PAGE - 16 * (lane >> 4);
 #pragma unroll
         for (int i = 0; i < LOADS; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(ring + slot * PAGE_BYTES + (wave * LOADS + i) * 1024), 16,
-                                                     lane * 16, (wave * LOADS + i) * 1024, 0, 0);
-        return scales[static_cast<size_t>(page) * a.kv_heads + w.head];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                int word = raw[i][j];
+                asm volatile("v_and_b32 %0, %1, %0" : "+v"(word) : "v"(low_bytes(valid - 4 * j)));       // in place: see the references' below
+                raw[i][j] = word;
+            }
+    };
+    auto put = [&](ldsptr to) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int at = piece + i, key_off = D == 128 ? (at & 1) * 4096 + (at >> 1) * 128 : at * 128, value_off = (at >> 1) * 4096 + (at & 1) * 256;
+            ldsptr dst = to + put_at + (brings_values ? value_off : key_off);
+            lds_put(dst, widen(raw[i][0], raw[i][1]));
+            lds_put(dst + 1024, widen(raw[i][2], raw[i][3]));
+        }
     };
 
     row_state state = {NOTHING, 0.f};
@@ -544,39 +576,60 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
     const bool capped = a.softcap > 0.f;
     const float in_unit = (capped ? 2.f * LOG2E * a.scale / a.softcap : a.scale * LOG2E) * q_unit, cap_out = a.softcap * LOG2E;
-    // where my chunks lie in a page: keys, tile u and dims 32 p + 16 h: rows of the tile are the keys 32 u + 16 (row / 4 % 2) + 4 (row / 8) + row % 4
-    const int key_at = ((n >> 3) * (D / 16) + h) * 256 + (n & 7) * 16, value_at = PAGE * D + ((n >> 4) * 4 + h) * 256 + (n & 15) * 16;
-
-    uint32_t sc[2] = {0, 0};                               // scales of the page that is read and of the next one
-    if (w.lo < w.hi) sc[0] = fetch(w.lo, 0);
-    if (w.lo + 1 < w.hi) sc[1] = fetch(w.lo + 1, 1);
-    int slot = 0;
-    for (int p = w.lo; p < w.hi; ++p) {
-        // page p is here once all but the loads of page p + 1 have arrived, everybody's once all waves are past this point; page p - 1 has been read then
-        // (the LDS reads of page p - 1 have returned before anybody's loads may overwrite it: lgkmcnt)
-        if (p + 1 < w.hi) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(LOADS) : "memory");
-        else              asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
-        const uint32_t now = sc[0];
-        sc[0] = sc[1];
-        if (p + 2 < w.hi) sc[1] = fetch(p + 2, slot + 2 >= RING ? slot + 2 - RING : slot + 2);
-        ldsptr here = ring + slot * PAGE_BYTES;
-        slot = slot + 1 == RING ? 0 : slot + 1;
-        if (!live || p * PAGE > high_token || (a.window > 0 && p * PAGE + PAGE <= low_token - a.window + 1)) continue;
-
-        // ---- scores
+    uint32_t now = 0;                                      // scales of the page that is read
+    if (w.lo < w.hi) {
+        now = fetch(w.lo);
+        clear_behind(w.lo);
+        put(ring);
+    }
+    // my rows see the pages [my_lo, my_hi) of the tile's; the others I only bring
+    const int my_hi = live ? max_of(min_of(w.hi, (high_token + PAGE) / PAGE), w.lo) : w.lo;
+    const int my_lo = min_of(my_hi, max_of(w.lo, a.window > 0 && low_token >= a.window ? (low_token - a.window + 1) / PAGE : 0));
+    int p = w.lo;
+    ldsptr here = ring + lane * 16, there = ring + 2 * PAGE_BYTES;           // the page that is read (for this lane), and the next one's place
+    auto turn = [&]() -> int {                             // page p is in the LDS once all waves are here, and page p - 1 has been read
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+        return min_of(p + 1, w.hi - 1);                    // the page to bring (the last one once more: no branch between its loads and their use)
+    };
+    auto swap = [&]() {
+        ldsptr t = here - lane * 16;
+        here = there + lane * 16;
+        there = t;
+        ++p;
+    };
+    auto only_bring = [&](int upto) {
+        while (p < upto) {
+            const int ahead = turn();
+            now = fetch(ahead);
+            clear_behind(ahead);
+            put(there);
+            swap();
+        }
+    };
+    only_bring(my_lo);
+    while (p < my_hi) {
+        const int ahead = turn();
         const page_scales ps = scales_of(now, p * PAGE + BLOCK < end);
+        now = fetch(ahead);
+        // ---- scores
         v16f z[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) z[u][i] = 0.f;
 #pragma unroll
-            for (int s = 0; s < QS; ++s) {
-                const v4i key = lds16(here + key_at + u * 128 + s * 512);
-                z[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen(key[0], key[1]), query[s][0], z[u], 0, 0, 0);
-                z[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen(key[2], key[3]), query[s][1], z[u], 0, 0, 0);
-            }
+            for (int s = 0; s < QS; ++s)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) z[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds8h(here + ((u * QS + s) * 2 + j) * 1024), query[s][j], z[u], 0, 0, 0);
         }
+        // the reads run a group of four ahead of the products
+        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+        for (int i = 0; i < QS - 2; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
         float unit[2] = {in_unit * ps.key[0], in_unit * ps.key[1]};          // of a score, to log 2
         if (capped) {
 #pragma unroll
@@ -589,31 +642,34 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
         if (p * PAGE + PAGE - 1 > low_token || (a.window > 0 && p * PAGE <= high_token - a.window)) {
             const int last = last_key - p * PAGE - 16 * h, from = first_key - p * PAGE - 16 * h;
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < 2; ++u) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) z[u][i] = 32 * u + i > last || 32 * u + i < from ? -INFINITY : z[u][i] * unit[u];
-            unit[0] = unit[1] = 1.f;
+                unit[u] = 1.f;
+            }
         }
-        // ---- weights
+        // ---- a reference that bears the largest of them
+        clear_behind(ahead);
         float top_of[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            top_of[u] = fmaxf(z[u][0], z[u][1]);
+            top_of[u] = z[u][0];
 #pragma unroll
-            for (int i = 2; i < 16; i += 2) top_of[u] = fmaxf(top_of[u], fmaxf(z[u][i], z[u][i + 1]));
+            for (int i = 1; i < 15; i += 2) top_of[u] = max3(top_of[u], z[u][i], z[u][i + 1]);
         }
-        float top = fmaxf(top_of[0] * unit[0], top_of[1] * unit[1]);
-        top = fmaxf(top, __shfl_xor(top, 32));
+        float top = max3(fmaxf(top_of[0], z[0][15]) * unit[0], fmaxf(top_of[1], z[1][15]) * unit[1], NOTHING);
         const int v_top = max_of(ps.value[0], ps.value[1]);
-        if (__ballot(top > state.ref + ABOVE || v_top > v_ref)) {
+        if (__ballot(top > state.ref + ABOVE) || v_top > v_ref) {
+            top = fmaxf(top, __shfl_xor(top, 32));         // the other half of the row
             const int to = max_of(v_ref, v_top);
             const float f = raise_reference(state, top) * __builtin_amdgcn_exp2f(static_cast<float>(v_ref - to));
             v_ref = to;
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) o[d][i] *= f;
+                for (int i = 0; i < 16; ++i) asm volatile("v_mul_f32 %0, %1, %0" : "+v"(o[d][i]) : "v"(f));      // in place: the usual way around has no copies to make
         }
+        // ---- weights and values
         v8h weights[2][2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -629,24 +685,33 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
             weights[u][0] = narrow(x);
             weights[u][1] = narrow(x + 8);
         }
-        // ---- values.  What lies behind the last token may be anything, a NaN too: cleared
-        auto add_values = [&](auto clear_tag) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    v4i value = lds16(here + value_at + d * 2048 + u * 512);
-                    if constexpr (decltype(clear_tag)::value) {
-                        const int valid = end - p * PAGE - BLOCK * u - 16 * h;
+                for (int j = 0; j < 2; ++j)
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds8h(here + VALUES + ((d * 2 + u) * 2 + j) * 1024), weights[u][j], o[d], 0, 0, 0);
+        put(there);
+        // the second tile's weights between the first tile's products, the next page's widening between the second's
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+        __builtin_amdgcn_sched_group_barrier(0x402, 60, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) value[j] &= low_bytes(valid - 4 * j);
-                    }
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen(value[0], value[1]), weights[u][0], o[d], 0, 0, 0);
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen(value[2], value[3]), weights[u][1], o[d], 0, 0, 0);
-                }
-        };
-        if (p * PAGE + PAGE > end) add_values(flag<true>{}); else add_values(flag<false>{});
+        for (int i = 0; i < 2 * DT; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x402, 56 / (2 * DT), 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * DT; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+            __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+        }
+        swap();
     }
+    only_bring(w.hi);
     const float v_unit = v_ref == NO_SCALE ? 0.f : exp2_int(v_ref);
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -728,7 +793,7 @@ __global__ __launch_bounds__(NT, 2) void attend_many_kernel(const epara_cache_at
                                                            const int32_t* __restrict__ pages, const int32_t* __restrict__ first, int n_seqs, int part_pages,
                                                            uint32_t* counters, char* slots)
 {
-    __shared__ __attribute__((aligned(1024))) char ring[RING * 2 * PAGE * 128];
+    __shared__ __attribute__((aligned(1024))) char ring[2 * 4 * PAGE * 128];        // two pages in f16: one is read, one on its way
     const int item = blockIdx.x;
     const work_item w = find_work<MANY_TILE>(args, seqs, first, n_seqs, part_pages, item, threadIdx.x & 63);
     if (w.part > 0 && w.part >= w.parts) return;
