@@ -614,14 +614,15 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
         // ---- scores
         v16f z[2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int i = 0; i < 16; ++i) z[u][i] = 0.f;
 #pragma unroll
-            for (int s = 0; s < QS; ++s)
+        for (int s = 0; s < QS; ++s)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) z[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds8h(here + ((u * QS + s) * 2 + j) * 1024), query[s][j], z[u], 0, 0, 0);
-        }
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) z[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds8h(here + ((u * QS + s) * 2 + j) * 1024), query[s][j], z[u], 0, 0, 0);
         // the reads run a group of four ahead of the products
         __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
 #pragma unroll
@@ -688,9 +689,9 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                for (int d = 0; d < DT; ++d)
                     o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds8h(here + VALUES + ((d * 2 + u) * 2 + j) * 1024), weights[u][j], o[d], 0, 0, 0);
         put(there);
         // the second tile's weights between the first tile's products, the next page's widening between the second's
