@@ -125,6 +125,7 @@ __device__ __forceinline__ v2f get2(const float* at)
 template <bool V> struct flag { static constexpr bool value = V; };
 constexpr float NOTHING = -1e30f;                          // reference of a row that has seen no key
 constexpr float ABOVE = 6.f, LIFT = 9.f;                   // a weight is at most 2^(ABOVE + LIFT) = 2^15
+constexpr float MOST = 32768.f;                            // sum of weights in which none can be more than that
 
 struct row_state { float ref, sum; };                      // M, and the sum of the weights relative to it (of this lane's keys)
 
@@ -151,14 +152,6 @@ __device__ __forceinline__ page_scales scales_of(uint32_t word, bool second_bloc
 }
 constexpr int NO_SCALE = -1000;                            // the values' reference before any page
 constexpr int LEAST_SHIFT = -60;                           // values under 2^-60 of the largest: their weights are zeros in f16, their sum still is fp32's
-
-// The largest of three; a NaN does not count.  (fmaxf first makes sure that its operands are no signalling NaNs: an instruction each.)
-__device__ __forceinline__ float max3(float a, float b, float c)
-{
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-    return r;
-}
 
 __device__ __forceinline__ float capped_score(float z, float in, float out)      // c tanh(z / c) = c (1 - 2 / (1 + e^(2 z / c))), in units of log 2
 {
@@ -552,9 +545,7 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
         for (int i = 0; i < LOADS; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                int word = raw[i][j];
-                asm volatile("v_and_b32 %0, %1, %0" : "+v"(word) : "v"(low_bytes(valid - 4 * j)));       // in place: see the references' below
-                raw[i][j] = word;
+                raw[i][j] &= low_bytes(valid - 4 * j);
             }
     };
     auto put = [&](ldsptr to) {
@@ -576,42 +567,45 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
     const bool capped = a.softcap > 0.f;
     const float in_unit = (capped ? 2.f * LOG2E * a.scale / a.softcap : a.scale * LOG2E) * q_unit, cap_out = a.softcap * LOG2E;
-    uint32_t now = 0;                                      // scales of the page that is read
+    // my rows see the pages [my_lo, my_hi) of the tile's; the others I only bring
+    const int my_hi = live ? max_of(min_of(w.hi, (high_token + PAGE) / PAGE), w.lo) : w.lo;
+    const int my_lo = min_of(my_hi, max_of(w.lo, a.window > 0 && low_token >= a.window ? (low_token - a.window + 1) / PAGE : 0));
+    uint32_t now = 0, next = 0;                            // scales of the page that is read and of the one in my registers
+    int p = w.lo;
+    ldsptr here = ring + lane * 16, there = ring + 2 * PAGE_BYTES;           // the page that is read (for this lane), and the next one's place
+    // page p lies in the LDS, page p + 1 in the registers of the waves that bring it (behind the last page: the last one once more, so that nothing branches)
+    auto page_or_last = [&](int i) { return min_of(i, w.hi - 1); };
     if (w.lo < w.hi) {
         now = fetch(w.lo);
         clear_behind(w.lo);
         put(ring);
+        next = fetch(page_or_last(w.lo + 1));
     }
-    // my rows see the pages [my_lo, my_hi) of the tile's; the others I only bring
-    const int my_hi = live ? max_of(min_of(w.hi, (high_token + PAGE) / PAGE), w.lo) : w.lo;
-    const int my_lo = min_of(my_hi, max_of(w.lo, a.window > 0 && low_token >= a.window ? (low_token - a.window + 1) / PAGE : 0));
-    int p = w.lo;
-    ldsptr here = ring + lane * 16, there = ring + 2 * PAGE_BYTES;           // the page that is read (for this lane), and the next one's place
-    auto turn = [&]() -> int {                             // page p is in the LDS once all waves are here, and page p - 1 has been read
+    auto turn = [&]() {                                    // page p is in the LDS once all waves are here, and page p - 1 has been read
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
-        return min_of(p + 1, w.hi - 1);                    // the page to bring (the last one once more: no branch between its loads and their use)
+        clear_behind(page_or_last(p + 1));
     };
     auto swap = [&]() {
         ldsptr t = here - lane * 16;
         here = there + lane * 16;
         there = t;
+        now = next;
         ++p;
     };
     auto only_bring = [&](int upto) {
         while (p < upto) {
-            const int ahead = turn();
-            now = fetch(ahead);
-            clear_behind(ahead);
+            turn();
             put(there);
+            const uint32_t later = fetch(page_or_last(p + 2));
             swap();
+            next = later;
         }
     };
     only_bring(my_lo);
     while (p < my_hi) {
-        const int ahead = turn();
+        turn();
         const page_scales ps = scales_of(now, p * PAGE + BLOCK < end);
-        now = fetch(ahead);
-        // ---- scores
+        // ---- scores; the next page's widening goes between the products
         v16f z[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
@@ -623,14 +617,16 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int u = 0; u < 2; ++u) z[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds8h(here + ((u * QS + s) * 2 + j) * 1024), query[s][j], z[u], 0, 0, 0);
-        // the reads run a group of four ahead of the products
+        put(there);
         __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
 #pragma unroll
-        for (int i = 0; i < QS - 2; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+        for (int i = 0; i < 4 * QS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if (i < 4 * QS - 8) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+            if (i & 1) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
         }
-        __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
+        const uint32_t later = fetch(page_or_last(p + 2));
         float unit[2] = {in_unit * ps.key[0], in_unit * ps.key[1]};          // of a score, to log 2
         if (capped) {
 #pragma unroll
@@ -649,68 +645,71 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
                 unit[u] = 1.f;
             }
         }
-        // ---- a reference that bears the largest of them
-        clear_behind(ahead);
-        float top_of[2];
+        auto scale_sums = [&](float f) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            top_of[u] = z[u][0];
-#pragma unroll
-            for (int i = 1; i < 15; i += 2) top_of[u] = max3(top_of[u], z[u][i], z[u][i + 1]);
-        }
-        float top = max3(fmaxf(top_of[0], z[0][15]) * unit[0], fmaxf(top_of[1], z[1][15]) * unit[1], NOTHING);
+            for (int d = 0; d < DT; ++d) o[d] *= f;
+        };
         const int v_top = max_of(ps.value[0], ps.value[1]);
-        if (__ballot(top > state.ref + ABOVE) || v_top > v_ref) {
-            top = fmaxf(top, __shfl_xor(top, 32));         // the other half of the row
-            const int to = max_of(v_ref, v_top);
-            const float f = raise_reference(state, top) * __builtin_amdgcn_exp2f(static_cast<float>(v_ref - to));
-            v_ref = to;
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) asm volatile("v_mul_f32 %0, %1, %0" : "+v"(o[d][i]) : "v"(f));      // in place: the usual way around has no copies to make
+        if (v_top > v_ref) {
+            scale_sums(__builtin_amdgcn_exp2f(static_cast<float>(v_ref - v_top)));
+            v_ref = v_top;
         }
-        // ---- weights and values
-        v8h weights[2][2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        // ---- weights of a tile, and their sum (of the rounded weights, two to an instruction).  The reference is raised only where the sum says that a weight may
+        // have left f16's range: no maximum is formed otherwise.  The first page's weights are infinite against NOTHING.
+        auto weigh = [&](int u, v8h* weights) -> float {
             const int v_shift = max_of(ps.value[u] - v_ref, LEAST_SHIFT);       // <= 0
             const float lift = LIFT - state.ref + static_cast<float>(v_shift);
-            float sum = 0.f, x[16];
+            float x[16], sum[2] = {0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                x[i] = __builtin_amdgcn_exp2f(fmaf(z[u][i], unit[u], lift));
-                sum += x[i];
+            for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(z[u][i], unit[u], lift));
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                weights[j] = narrow(x + 8 * j);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[j] = __builtin_amdgcn_fdot2(v2h{weights[j][2 * i], weights[j][2 * i + 1]}, v2h{1, 1}, sum[j], false);
             }
-            state.sum += sum * exp2_int(-v_shift);
-            weights[u][0] = narrow(x);
-            weights[u][1] = narrow(x + 8);
-        }
+            return (sum[0] + sum[1]) * exp2_int(-v_shift);
+        };
+        auto raise = [&](int u) {
+            float top = z[u][0];
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+            for (int i = 1; i < 16; ++i) top = fmaxf(top, z[u][i]);
+            top *= unit[u];
+            top = fmaxf(top, __shfl_xor(top, 32));         // the other half of the row
+            scale_sums(raise_reference(state, top));
+        };
+        auto add_values = [&](int u, const v8h* weights) {
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds8h(here + VALUES + ((d * 2 + u) * 2 + j) * 1024), weights[u][j], o[d], 0, 0, 0);
-        put(there);
-        // the second tile's weights between the first tile's products, the next page's widening between the second's
-        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-        __builtin_amdgcn_sched_group_barrier(0x402, 60, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds8h(here + VALUES + ((d * 2 + u) * 2 + j) * 1024), weights[j], o[d], 0, 0, 0);
+        };
+        v8h first[2], second[2];
+        float sum = weigh(0, first);
+        if (__ballot(sum > MOST)) {
+            raise(0);
+            sum = weigh(0, first);
+        }
+        state.sum += sum;
+        add_values(0, first);
+        sum = weigh(1, second);
+        // the second tile's weights between the first tile's products
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 1);
 #pragma unroll
         for (int i = 0; i < 2 * DT; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x402, 56 / (2 * DT), 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+            __builtin_amdgcn_sched_group_barrier(0x402, 56 / (2 * DT), 1);
+            if (i < 2 * DT - 4) __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
         }
-#pragma unroll
-        for (int i = 0; i < 2 * DT; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
-            __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+        if (__ballot(sum > MOST)) {
+            raise(1);
+            sum = weigh(1, second);
         }
+        state.sum += sum;
+        add_values(1, second);
         swap();
+        next = later;
     }
     only_bring(w.hi);
     const float v_unit = v_ref == NO_SCALE ? 0.f : exp2_int(v_ref);
