@@ -346,6 +346,20 @@ def epara_attention(h_args, d_args, stream=0):
            "epara_attention")
 
 
+class Call:
+    """An entry point with all of its arguments but the stream: what a plan keeps, so that a call costs no marshalling.  The plan keeps alive what
+    the arguments point to."""
+    __slots__ = ("name", "fn", "args")
+
+    def __init__(self, name, *args):
+        self.name, self.fn, self.args = name, getattr(lib(), name), args
+
+    def __call__(self, stream=0):
+        status = self.fn(*self.args, stream or None)
+        if status != EPARA_OK:
+            raise EparaError(status, self.name)
+
+
 def epara_add_rmsnorm(h_args, d_args, out_dtype, stream=0):
     """h_args: RMSNORM_ARGS[G] (host copy, validated); d_args: device address of the same bytes."""
     h_args = np.ascontiguousarray(h_args, dtype=RMSNORM_ARGS)

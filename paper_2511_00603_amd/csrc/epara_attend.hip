@@ -158,6 +158,31 @@ __device__ __forceinline__ float capped_score(float z, float in, float out)     
     return out - 2.f * out * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * in));
 }
 
+// The page numbers and scales of 64 pages of a part, one to a lane: a page costs two register reads instead of two dependent trips to memory.
+// (Scalar loads would have every wait for the LDS wait for them too.)
+struct page_list {
+    const EPARA_GLOBAL int32_t* table;
+    const EPARA_GLOBAL uint32_t* scales;
+    int kv_heads, head, hi;
+    int base, id;
+    uint32_t word;
+    __device__ __forceinline__ void fill(int from, int lane)
+    {
+        base = from;
+        id = table[min_of(from + lane, hi - 1)];
+        word = scales[static_cast<size_t>(static_cast<uint32_t>(id)) * kv_heads + head];
+    }
+    __device__ __forceinline__ void reach(int p, int lane) { if (p - base >= 64) fill(p, lane); }
+    __device__ __forceinline__ uint32_t page(int p) const { return __builtin_amdgcn_readlane(id, p - base); }
+    __device__ __forceinline__ uint32_t scale_word(int p) const { return __builtin_amdgcn_readlane(word, p - base); }
+};
+__device__ __forceinline__ page_list pages_of(const work_item& w, const int32_t* pages, int lane)
+{
+    page_list l = {(const EPARA_GLOBAL int32_t*)pages + w.s.first_page, (const EPARA_GLOBAL uint32_t*)w.a.scales, w.a.kv_heads, w.head, w.hi, w.lo, 0, 0};
+    if (w.lo < w.hi) l.fill(w.lo, lane);
+    return l;
+}
+
 template <int D>
 struct few_lds {
     union {
@@ -293,7 +318,7 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
     const size_t page_bytes = static_cast<size_t>(a.kv_heads) * head_bytes(D);
     v4i k[4][KS], v[D / 16];
     uint32_t scales = 0, scales_next = 0;
-    auto base_of = [&](int page) { return (const EPARA_GLOBAL char*)a.codes + static_cast<size_t>(page) * page_bytes + head_offset + lane * 16; };
+    auto base_of = [&](uint32_t page) { return (const EPARA_GLOBAL char*)a.codes + static_cast<size_t>(page) * page_bytes + head_offset + lane * 16; };
     auto load_keys = [&](const EPARA_GLOBAL char* base) {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -304,8 +329,7 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) v[d] = __builtin_nontemporal_load(reinterpret_cast<const EPARA_GLOBAL v4i*>(base + PAGE * D + d * 1024));
     };
-    auto page_at = [&](int p) { return __builtin_amdgcn_readfirstlane(pages[w.s.first_page + p]); };
-    auto scale_word = [&](int page) { return ((const EPARA_GLOBAL uint32_t*)a.scales)[static_cast<size_t>(page) * a.kv_heads + w.head]; };
+    page_list list = pages_of(w, pages, lane);
 
     row_state state = {NOTHING, 0.f};
     int v_ref = NO_SCALE;
@@ -318,9 +342,9 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
     int p = w.lo + wave;
     const EPARA_GLOBAL char* base = nullptr;
     if (p < w.hi) {
-        const int page = page_at(p);
-        base = base_of(page);
-        scales = scale_word(page);
+        list.reach(p, lane);
+        base = base_of(list.page(p));
+        scales = list.scale_word(p);
         load_keys(base);
         load_values(base);
     }
@@ -328,9 +352,9 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
         const bool more = p + WAVES < w.hi;
         const EPARA_GLOBAL char* next = base;
         if (more) {
-            const int page = page_at(p + WAVES);
-            next = base_of(page);
-            scales_next = scale_word(page);
+            list.reach(p + WAVES, lane);
+            next = base_of(list.page(p + WAVES));
+            scales_next = list.scale_word(p + WAVES);
         }
         // ---- scores
         const page_scales ps = scales_of(scales, p * PAGE + BLOCK < end);
@@ -477,7 +501,6 @@ __global__ __launch_bounds__(NT, 2) void attend_few_kernel(const epara_cache_att
 // ---- many rows -------------------------------------------------------------------------------------------------
 
 typedef __attribute__((address_space(3))) char* ldsptr;
-typedef const __attribute__((address_space(4))) uint32_t* constant_words;
 __device__ __forceinline__ v8h lds8h(ldsptr at) { return *reinterpret_cast<const __attribute__((address_space(3))) v8h*>(at); }
 __device__ __forceinline__ void lds_put(ldsptr at, v8h x) { *reinterpret_cast<__attribute__((address_space(3))) v8h*>(at) = x; }
 
@@ -523,8 +546,7 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
 
     // ---- pages to the LDS, widened on the way: a wave brings a quarter of each, waves 0 and 1 the keys.  A page in the LDS is in f16, in pieces of
     // 1 KiB of which lane l reads 16 bytes at 16 l: keys (tile u, dims 32 s + 16 h + 8 j ..), then values (dims 32 d .., tile u, tokens 16 h + 8 j ..)
-    const constant_words table = (constant_words)(pages + w.s.first_page);
-    const constant_words scales = (constant_words)a.scales;
+    page_list list = pages_of(w, pages, lane);
     const size_t page_bytes = static_cast<size_t>(a.kv_heads) * PAGE_BYTES;
     const bool brings_values = wave >= 2;
     const int piece = (wave & 1) * LOADS;                  // of its half of the page
@@ -532,11 +554,11 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
                                      : ((lane >> 3) & 1) * (D * 64) + (lane >> 5) * 2048 + ((lane >> 4) & 1) * 512 + (lane & 7) * 16;
     v4i raw[LOADS];
     auto fetch = [&](int p) -> uint32_t {                  // returns the page's scales
-        const uint32_t page = table[p];
-        const EPARA_GLOBAL char* base = (const EPARA_GLOBAL char*)a.codes + page * page_bytes + static_cast<size_t>(w.head) * PAGE_BYTES + wave * LOADS * 1024 + lane * 16;
+        list.reach(p, lane);
+        const EPARA_GLOBAL char* base = (const EPARA_GLOBAL char*)a.codes + list.page(p) * page_bytes + static_cast<size_t>(w.head) * PAGE_BYTES + wave * LOADS * 1024 + lane * 16;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) raw[i] = *reinterpret_cast<const EPARA_GLOBAL v4i*>(base + i * 1024);
-        return scales[static_cast<size_t>(page) * a.kv_heads + w.head];
+        return list.scale_word(p);
     };
     auto clear_behind = [&](int p) {                       // values behind the last token may be anything, a NaN too
         if (!brings_values || p * PAGE + PAGE <= end) return;
@@ -605,7 +627,7 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
     while (p < my_hi) {
         turn();
         const page_scales ps = scales_of(now, p * PAGE + BLOCK < end);
-        // ---- scores; the next page's widening goes between the products
+        // ---- scores, and the next page's widening
         v16f z[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
@@ -618,14 +640,6 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
 #pragma unroll
                 for (int u = 0; u < 2; ++u) z[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds8h(here + ((u * QS + s) * 2 + j) * 1024), query[s][j], z[u], 0, 0, 0);
         put(there);
-        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-#pragma unroll
-        for (int i = 0; i < 4 * QS; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            if (i < 4 * QS - 8) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
-            if (i & 1) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
-        }
         const uint32_t later = fetch(page_or_last(p + 2));
         float unit[2] = {in_unit * ps.key[0], in_unit * ps.key[1]};          // of a score, to log 2
         if (capped) {
@@ -694,14 +708,6 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
         state.sum += sum;
         add_values(0, first);
         sum = weigh(1, second);
-        // the second tile's weights between the first tile's products
-        __builtin_amdgcn_sched_group_barrier(0x100, 4, 1);
-#pragma unroll
-        for (int i = 0; i < 2 * DT; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
-            __builtin_amdgcn_sched_group_barrier(0x402, 56 / (2 * DT), 1);
-            if (i < 2 * DT - 4) __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
-        }
         if (__ballot(sum > MOST)) {
             raise(1);
             sum = weigh(1, second);
