@@ -2,7 +2,7 @@
 //
 //   s = x + r,  y = s / sqrt(mean(s^2) + eps) * gamma;   8 bits: code = sat(RNE(y / scale))
 //
-// A wave per row: the row is read once and stays in registers; its sum of squares and (8 bits with a scale per row) the
+// A wave or a workgroup per row: the row is read once and stays in registers; its sum of squares and (8 bits with a scale per row) the
 // maximum of |s gamma| are reduced together, since max |y| = max |s gamma| / sqrt(..).
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -21,7 +21,7 @@ typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 #define EPARA_GLOBAL __attribute__((address_space(1)))
 
 constexpr int NT = 256;
-constexpr int NORM_GRID = 1024;
+constexpr int NORM_GRID = 2048;
 
 __device__ __forceinline__ float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
@@ -42,59 +42,84 @@ __device__ __forceinline__ int find_group(const epara_rmsnorm_args* __restrict__
     return lo;
 }
 
-// CH = 16-byte chunks (8 values) per lane that the widest row of the launch needs.
-template <int CH, bool BITS8>
+// THREADS threads share a row (64: a wave, narrow rows; 256: a workgroup), CH = 16-byte chunks (8 values) of it per thread that the widest row of
+// the launch needs.  The loads of the next row are in flight while one is reduced and stored, and gamma stays in registers for as long as the
+// rows are of one service.
+template <int THREADS, int CH, bool BITS8>
 __global__ __launch_bounds__(NT) void add_rmsnorm_kernel(const epara_rmsnorm_args* __restrict__ args, int G, int n_rows)
 {
+    constexpr int ROWS = NT / THREADS, WAVES = THREADS / 64;
+    __shared__ float part[2][2][WAVES];                    // [turn][sum, maximum][wave]
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int at = THREADS == 64 ? lane : static_cast<int>(threadIdx.x);           // my place in the row
     const int first = G <= 64 && lane < G ? args[lane].first_row : 0x7fffffff;
-    for (long next = static_cast<long>(blockIdx.x) * (NT / 64) + wave; next < n_rows; next += gridDim.x * (NT / 64)) {
-        const int global_row = static_cast<int>(next);
-        const epara_rmsnorm_args a = args[__builtin_amdgcn_readfirstlane(find_group(args, G, global_row, first))];
-        const int row = global_row - a.first_row, n_chunks = a.d >> 3;
-        const size_t base = static_cast<size_t>(row) * a.d;
-        const EPARA_GLOBAL char* x = (const EPARA_GLOBAL char*)a.X + base * 2;
-        const EPARA_GLOBAL char* r = a.R ? (const EPARA_GLOBAL char*)a.R + base * 2 : nullptr;
-        const EPARA_GLOBAL float* gamma = (const EPARA_GLOBAL float*)a.gamma;
-        float s[CH][8];
-        float sum = 0.f, top = 0.f;
-        v4i xv[CH], rv[CH];
+    const int stride = gridDim.x * ROWS;
+    v4i xv[CH], rv[CH];
+    epara_rmsnorm_args a;
+    auto load = [&](int global_row, epara_rmsnorm_args& q, int& group) {
+        group = __builtin_amdgcn_readfirstlane(find_group(args, G, global_row, first));
+        q = args[group];
+        const size_t base = static_cast<size_t>(global_row - q.first_row) * q.d * 2;
+        const EPARA_GLOBAL char* x = (const EPARA_GLOBAL char*)q.X + base;
+        const EPARA_GLOBAL char* r = q.R ? (const EPARA_GLOBAL char*)q.R + base : nullptr;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int chunk = c * 64 + lane;
+            const int chunk = c * THREADS + at;
             xv[c] = v4i{0, 0, 0, 0};
             rv[c] = v4i{0, 0, 0, 0};
-            if (chunk < n_chunks) {
+            if (chunk < q.d >> 3) {
                 xv[c] = *reinterpret_cast<const EPARA_GLOBAL v4i*>(x + chunk * 16);
                 if (r) rv[c] = *reinterpret_cast<const EPARA_GLOBAL v4i*>(r + chunk * 16);
             }
         }
+    };
+    int row = blockIdx.x * ROWS + (THREADS == 64 ? wave : 0);
+    if (row >= n_rows) return;                             // (a whole wave, or a whole workgroup)
+    int group, gamma_of = -1, turn = 0;
+    load(row, a, group);
+    v4f gm[CH][2];
+    for (;;) {
+        const int n_chunks = a.d >> 3;
+        if (group != gamma_of) {
+            gamma_of = group;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int chunk = c * 64 + lane;
+            for (int c = 0; c < CH; ++c)
+                if (c * THREADS + at < n_chunks) {
+                    const EPARA_GLOBAL float* gamma = (const EPARA_GLOBAL float*)a.gamma + (c * THREADS + at) * 8;
+                    gm[c][0] = *reinterpret_cast<const EPARA_GLOBAL v4f*>(gamma);
+                    gm[c][1] = *reinterpret_cast<const EPARA_GLOBAL v4f*>(gamma + 4);
+                }
+        }
+        float s[CH][8], sum = 0.f, top = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const uint32_t xu = static_cast<uint32_t>(xv[c][j]), ru = static_cast<uint32_t>(rv[c][j]);
-                s[c][2 * j] = bf16_lo(xu) + bf16_lo(ru);
+                s[c][2 * j] = bf16_lo(xu) + bf16_lo(ru);   // chunks past the row hold zeros and add nothing
                 s[c][2 * j + 1] = bf16_hi(xu) + bf16_hi(ru);
                 sum += s[c][2 * j] * s[c][2 * j] + s[c][2 * j + 1] * s[c][2 * j + 1];
             }
+        const epara_rmsnorm_args now = a;
+        const size_t base = static_cast<size_t>(row - now.first_row) * now.d;
+        const int row_of_group = row - now.first_row, next = row + stride;
+        const bool more = next < n_rows && next > row;     // (a sum past 2^31 is negative)
+        if (more) load(next, a, group);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int chunk = c * THREADS + at;
             if (chunk >= n_chunks) continue;
-            if (a.S) {
+            if (now.S) {
                 v4i out;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) out[j] = static_cast<int>(pack_bf16(s[c][2 * j], s[c][2 * j + 1]));
-                *reinterpret_cast<EPARA_GLOBAL v4i*>((EPARA_GLOBAL char*)a.S + base * 2 + chunk * 16) = out;
+                *reinterpret_cast<EPARA_GLOBAL v4i*>((EPARA_GLOBAL char*)now.S + base * 2 + chunk * 16) = out;
             }
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const v4f gm = *reinterpret_cast<const EPARA_GLOBAL v4f*>(gamma + chunk * 8 + h * 4);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    s[c][4 * h + j] *= gm[j];
-                    if constexpr (BITS8) top = fmaxf(top, fabsf(s[c][4 * h + j]));
-                }
+            for (int j = 0; j < 8; ++j) {
+                s[c][j] *= gm[c][j >> 2][j & 3];
+                if constexpr (BITS8) top = fmaxf(top, fabsf(s[c][j]));
             }
         }
 #pragma unroll
@@ -102,46 +127,68 @@ __global__ __launch_bounds__(NT) void add_rmsnorm_kernel(const epara_rmsnorm_arg
             sum += __shfl_xor(sum, d);
             if constexpr (BITS8) top = fmaxf(top, __shfl_xor(top, d));
         }
-        const float rms = 1.f / sqrtf(sum / static_cast<float>(a.d) + a.eps);
-        float factor = rms;
+        if constexpr (WAVES > 1) {                         // the turns alternate, so the next row's sums do not overtake a slow wave's reads
+            if (lane == 0) {
+                part[turn][0][wave] = sum;
+                part[turn][1][wave] = top;
+            }
+            __syncthreads();
+            sum = part[turn][0][0];
+            top = part[turn][1][0];
+#pragma unroll
+            for (int i = 1; i < WAVES; ++i) {
+                sum += part[turn][0][i];
+                if constexpr (BITS8) top = fmaxf(top, part[turn][1][i]);
+            }
+            turn ^= 1;
+        }
+        float factor = 1.f / sqrtf(sum / static_cast<float>(now.d) + now.eps);
         if constexpr (BITS8) {
-            float inv = a.out_inv_scale;
-            if (a.row_scales) {
-                const float scale = top * rms == 0.f ? 1.f : top * rms / 448.f;          // a NaN in the row is a NaN here
+            float inv = now.out_inv_scale;
+            if (now.row_scales) {
+                const float scale = top * factor == 0.f ? 1.f : top * factor / 448.f;    // a NaN in the row is a NaN here
                 inv = 1.f / scale;
-                if (lane == 0) ((EPARA_GLOBAL float*)a.row_scales)[row] = scale;
+                if (at == 0) ((EPARA_GLOBAL float*)now.row_scales)[row_of_group] = scale;
             }
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                const int chunk = c * 64 + lane;
+                const int chunk = c * THREADS + at;
                 if (chunk >= n_chunks) continue;
                 float y[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) y[j] = s[c][j] * factor * inv;
                 const v2u codes = {epara_cast::f32x4_to_e4m3(y[0], y[1], y[2], y[3]), epara_cast::f32x4_to_e4m3(y[4], y[5], y[6], y[7])};
-                *reinterpret_cast<EPARA_GLOBAL v2u*>((EPARA_GLOBAL char*)a.Y + base + chunk * 8) = codes;
+                *reinterpret_cast<EPARA_GLOBAL v2u*>((EPARA_GLOBAL char*)now.Y + base + chunk * 8) = codes;
             }
         } else {
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                const int chunk = c * 64 + lane;
+                const int chunk = c * THREADS + at;
                 if (chunk >= n_chunks) continue;
                 v4i out;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) out[j] = static_cast<int>(pack_bf16(s[c][2 * j] * factor, s[c][2 * j + 1] * factor));
-                *reinterpret_cast<EPARA_GLOBAL v4i*>((EPARA_GLOBAL char*)a.Y + base * 2 + chunk * 16) = out;
+                *reinterpret_cast<EPARA_GLOBAL v4i*>((EPARA_GLOBAL char*)now.Y + base * 2 + chunk * 16) = out;
             }
         }
+        if (!more) return;
+        row = next;
     }
 }
 
 template <bool BITS8>
-void enqueue(int per_lane, int grid, hipStream_t s, const epara_rmsnorm_args* d_args, int G, int rows)
+void enqueue(int widest, int rows, hipStream_t s, const epara_rmsnorm_args* d_args, int G)
 {
-    if (per_lane <= 2)      hipLaunchKernelGGL((add_rmsnorm_kernel<2, BITS8>), dim3(grid), dim3(NT), 0, s, d_args, G, rows);
-    else if (per_lane <= 4) hipLaunchKernelGGL((add_rmsnorm_kernel<4, BITS8>), dim3(grid), dim3(NT), 0, s, d_args, G, rows);
-    else if (per_lane <= 8) hipLaunchKernelGGL((add_rmsnorm_kernel<8, BITS8>), dim3(grid), dim3(NT), 0, s, d_args, G, rows);
-    else                    hipLaunchKernelGGL((add_rmsnorm_kernel<16, BITS8>), dim3(grid), dim3(NT), 0, s, d_args, G, rows);
+    const int per_lane = (widest + 511) >> 9, per_thread = (widest + 2047) >> 11;
+    const bool narrow = per_lane <= 2;
+    const int items = narrow ? static_cast<int>((static_cast<int64_t>(rows) + NT / 64 - 1) / (NT / 64)) : rows;
+    const dim3 grid(items < NORM_GRID ? items : NORM_GRID), wg(NT);
+    if (per_lane <= 1)        hipLaunchKernelGGL((add_rmsnorm_kernel<64, 1, BITS8>), grid, wg, 0, s, d_args, G, rows);
+    else if (narrow)          hipLaunchKernelGGL((add_rmsnorm_kernel<64, 2, BITS8>), grid, wg, 0, s, d_args, G, rows);
+    else if (per_thread <= 1) hipLaunchKernelGGL((add_rmsnorm_kernel<256, 1, BITS8>), grid, wg, 0, s, d_args, G, rows);
+    else if (per_thread <= 2) hipLaunchKernelGGL((add_rmsnorm_kernel<256, 2, BITS8>), grid, wg, 0, s, d_args, G, rows);
+    else if (per_thread <= 3) hipLaunchKernelGGL((add_rmsnorm_kernel<256, 3, BITS8>), grid, wg, 0, s, d_args, G, rows);
+    else                      hipLaunchKernelGGL((add_rmsnorm_kernel<256, 4, BITS8>), grid, wg, 0, s, d_args, G, rows);
 }
 
 inline bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
@@ -171,11 +218,8 @@ extern "C" int32_t epara_add_rmsnorm(const epara_rmsnorm_args* h_args, const epa
         if (rows > INT32_MAX) return EPARA_ERR_SHAPE;
     }
     if (rows == 0) return EPARA_OK;
-    const int64_t groups_of_rows = (rows + NT / 64 - 1) / (NT / 64);
-    const int grid = static_cast<int>(groups_of_rows < NORM_GRID ? groups_of_rows : NORM_GRID);
-    const int per_lane = (widest + 511) >> 9;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (bits8) enqueue<true>(per_lane, grid, s, d_args, G, static_cast<int>(rows));
-    else       enqueue<false>(per_lane, grid, s, d_args, G, static_cast<int>(rows));
+    if (bits8) enqueue<true>(widest, static_cast<int>(rows), s, d_args, G);
+    else       enqueue<false>(widest, static_cast<int>(rows), s, d_args, G);
     return hipGetLastError() == hipSuccess ? EPARA_OK : EPARA_ERR_HIP;
 }
