@@ -60,6 +60,19 @@ class BlockParams:
 
 
 @dataclass
+class DecoderParams:
+    """What a SwiGLU service needs besides its FFN to run a whole pre-norm decoder block."""
+    Wqkv: np.ndarray              # fp32 [d, (heads + 2 kv_heads) * head_dim]
+    Wproj: np.ndarray             # fp32 [heads * head_dim, d]
+    gamma1: np.ndarray            # fp32 [d]: scale of the normalisation before attention, and of the one before the FFN
+    gamma2: np.ndarray
+    heads: int
+    kv_heads: int
+    head_dim: int
+    eps: float
+
+
+@dataclass
 class Mix:
     index: int
     name: str
@@ -189,4 +202,18 @@ def make_vit_block(mix, seed=SEED, eps=1e-6):
         g1, b1 = (1.0 + _normal(rng, (d,), 0.1)).astype(np.float32), _normal(rng, (d,), 0.1)
         g2, b2 = (1.0 + _normal(rng, (d,), 0.1)).astype(np.float32), _normal(rng, (d,), 0.1)
         out.append(BlockParams(proj, g1, b1, g2, b2, d // 64, svc.request_rows[0], eps))
+    return out
+
+
+def make_decoder_block(mix, kv_heads=8, head_dim=128, seed=SEED, eps=1e-5):
+    """Per service of a decode or prefill mix (index 4 or 5, any size): the rest of a decoder block's parameters, from a generator of their own
+    (the mix's draws stay what they are): projections W ~ N(0, 1/fan_in) without bias, scales 1 + N(0, 0.1); d / head_dim query heads."""
+    rng = np.random.default_rng([seed, mix.index, 2])
+    out = []
+    for svc in mix.services:
+        d = svc.X.shape[1]
+        heads = d // head_dim
+        qkv, proj = _dense(rng, d, (heads + 2 * kv_heads) * head_dim, "none", False), _dense(rng, heads * head_dim, d, "none", False)
+        g1, g2 = ((1.0 + _normal(rng, (d,), 0.1)).astype(np.float32) for _ in range(2))
+        out.append(DecoderParams(qkv.W, proj.W, g1, g2, heads, kv_heads, head_dim, eps))
     return out
