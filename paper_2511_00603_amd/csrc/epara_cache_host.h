@@ -16,11 +16,16 @@ EPARA_HIDDEN int32_t epara_check_copy_call(const epara_page_copy* caches, int32_
 inline int64_t epara_attn_counter_bytes(const int32_t n_items[2]) { return ((static_cast<int64_t>(n_items[0]) + n_items[1]) * 4 + 255) & ~static_cast<int64_t>(255); }
 
 // Pages to a workgroup.  work: pages x key heads that the tiles of each kind see; longest: pages that one tile sees at most.
+// Few rows: one workgroup to a compute unit where the work is small (one request at 32768 tokens, 33 / 17 / 9 / 4 pages to a workgroup: 22.7 / 20.0 / 23.2 / 23.9 us; 4 at
+// 8192: 21.9 / 17.5 / 18.3 / 22.4), at most 64 pages (16 requests at 16384: 64 pages 86 us, 17 97 us).  Many rows: two to a unit, at least 16 pages, since a part
+// costs 64 KiB there and back (two pieces of 256 rows at 8000 tokens, at least 4 / 8 / 16 / 32 pages: 46 / 47 / 36 / 50 us; three pieces of
+// 257 to 512 tokens at 3000 to 7000, 64 / 38 / 19 / 13 pages: 195 / 140 / 142 / 135 us).
 inline void epara_attn_part_pages(const int64_t work[2], const int64_t longest[2], int32_t n_compute_units, int32_t part_pages[2])
 {
     for (int k = 0; k < 2; ++k) {
-        const int64_t even = work[k] / ((k + 1) * static_cast<int64_t>(n_compute_units)) + 1, least = (longest[k] + epara_cache::MAX_PARTS - 1) / epara_cache::MAX_PARTS;
-        const int64_t part = even < 4 ? 4 : even > 64 ? 64 : even;
+        const int64_t slots = (k + 1) * static_cast<int64_t>(n_compute_units), fewest = k ? 16 : 4;
+        const int64_t even = work[k] / slots + 1, part = even < fewest ? fewest : even > 64 ? 64 : even;
+        const int64_t least = (longest[k] + epara_cache::MAX_PARTS - 1) / epara_cache::MAX_PARTS;
         part_pages[k] = static_cast<int32_t>(part < least ? least : part);
     }
 }
