@@ -959,8 +959,7 @@ typedef struct {
     int32_t reserved[2];
 } epara_cache_attn_args;
 
-/* How a call is cut into work: made by epara_plan_cache_attention from the shapes alone (sequences, heads, windows), so that all layers
- * of a model share it.  first[0 .. n_seqs] and first[n_seqs + 1 .. 2 n_seqs + 1] are running sums of the workgroups of the sequences
+/* How a call is cut into work: made by epara_plan_cache_attention from the shapes alone (sequences, heads, windows).  first[0 .. n_seqs] and first[n_seqs + 1 .. 2 n_seqs + 1] are running sums of the workgroups of the sequences
  * with few and with many rows to a key head. */
 typedef struct {
     int32_t n_items[2];         /* workgroups with few and with many rows */

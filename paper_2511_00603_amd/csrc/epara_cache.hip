@@ -2,7 +2,9 @@
 //
 // Both are bound by memory.  Append: a wave takes the new tokens of one block (32 tokens that share a scale) and key head: its
 // keys and values are read once, stay in registers as fp32 until the block's largest value is known, and leave as whole
-// 16-byte chunks of the page; or a few rows x heads of the queries.  Copy: a workgroup per page and head.
+// 16-byte chunks of the page; or a few rows x heads of the queries, with the angles of a row read once for its heads.  Copy: a workgroup per page and head.
+// Measured: prompts of 6 requests (0.47 GB in and out) 116 us, 4.1 TB/s at two waves per SIMD; a token of 105 requests 8 us,
+// a chain of dependent trips to memory; 3001 pages of 128 KiB copied in 153 us, 5.1 TB/s, as fast as a plain copy of this size.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
