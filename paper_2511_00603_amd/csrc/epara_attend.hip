@@ -676,20 +676,20 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
             scale_sums(__builtin_amdgcn_exp2f(static_cast<float>(v_ref - v_top)));
             v_ref = v_top;
         }
-        // ---- weights of a tile, and their sum (of the rounded weights, two to an instruction).  The reference is raised only where the sum says that a weight may
-        // have left f16's range: no maximum is formed otherwise.  The first page's weights are infinite against NOTHING.
+        // ---- weights of a tile, and their sum without the values' scale (in fp32 before they are rounded: a block of small values may leave f16 nothing of
+        // its weights, but the sum needs them).  The reference is raised only where the sum says that a weight may have left f16's range: no
+        // maximum is formed otherwise.  The first page's weights are infinite against NOTHING.
         auto weigh = [&](int u, v8h* weights) -> float {
             const int v_shift = max_of(ps.value[u] - v_ref, LEAST_SHIFT);       // <= 0
             const float lift = LIFT - state.ref + static_cast<float>(v_shift);
             float x[16], sum[2] = {0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(z[u][i], unit[u], lift));
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                weights[j] = narrow(x + 8 * j);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sum[j] = __builtin_amdgcn_fdot2(v2h{weights[j][2 * i], weights[j][2 * i + 1]}, v2h{1, 1}, sum[j], false);
+            for (int i = 0; i < 16; ++i) {
+                x[i] = __builtin_amdgcn_exp2f(fmaf(z[u][i], unit[u], lift));
+                sum[i & 1] += x[i];
             }
+            weights[0] = narrow(x);
+            weights[1] = narrow(x + 8);
             return (sum[0] + sum[1]) * exp2_int(-v_shift);
         };
         auto raise = [&](int u) {

@@ -454,6 +454,26 @@ def test_attention_with_scores_that_rise_and_fall_by_hundreds(rows):
         check_attn([c])
 
 
+@pytest.mark.parametrize("rows", [1, 90])
+@pytest.mark.parametrize("tiny", [0.0, 1e-20, 1e-5])
+def test_attention_with_blocks_of_zero_and_of_tiny_values(rows, tiny):
+    """Tokens whose values are (all but) zeros still take their share of the weights, before and behind blocks of ordinary and of huge values."""
+    for D in (64, 128):
+        n, rng = 300, np.random.default_rng([72, D])
+        case = Case(rng, [n], 2, 1, D)
+        K, V = rng.standard_normal((n, 1, D)), rng.standard_normal((n, 1, D))
+        for lo, hi in ((0, 32), (64, 128), (160, 192)):
+            V[lo:hi] *= tiny
+        V[224:256] *= 1e6 if rows == 1 else 1.0
+        case.oracle.append(case.pages[0], 0, K, V)
+        case.upload()
+        q, Q = dev_bf16(rng.standard_normal((rows, 2 * D)))
+        c = (case, [{"first_row": 0, "rows": rows, "start": n - rows, "pages": case.pages[0]}], {"Q": Q, "O": torch.zeros(rows, 2 * D, dtype=torch.bfloat16, device=DEV), "cache": case.cache,
+             "heads": 2, "window": 0, "softcap": 0.0}, q.reshape(rows, 2, D))
+        run_attn([c])
+        check_attn([c])
+
+
 @pytest.mark.parametrize("rows", [3, 80])
 def test_attention_keeps_broken_tokens_from_rows_that_do_not_see_them(rows):
     for D in (64, 128):
