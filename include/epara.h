@@ -984,9 +984,9 @@ typedef struct {
  *   z_j = scale * q . k_j (capped: softcap * tanh(z_j / softcap)), o = sum_j exp(z_j - m) v_j / sum_j exp(z_j - m), m = max_j z_j.
  * A row at a negative position gets zeros.  Both products run on the matrix cores in f16 with fp32 sums: codes widen to f16 exactly,
  * a query does once its head's own power of two is taken out (but for what lies under 2^-22 of its largest value), and a weight keeps 11
- * bits (down to 2^-23 of its row's largest; 2^-33 is the last that counts); maxima, exponentials and the weights' sums are fp32.  Values
- * are held relative to the largest scale among the pages that a workgroup reads: a block's weights lose bits where its values lie under
- * 2^-10 of that.  One kernel for sequences with few rows to a key head, one for those with many; a long context is cut into parts that
+ * bits; maxima, exponentials and the weights' sums are fp32.  Weights are held relative to what the row gets most of: of all keys that it sees,
+ * the largest weight times its block's scale.  They keep their bits down to 2^-23 of that, and 2^-33 is the last that counts; keys that a row does
+ * not see take no part.  One kernel for sequences with few rows to a key head, one for those with many; a long context is cut into parts that
  * run side by side, and the last of them to end adds them up in order: results do not depend on timing.
  * Errors as for epara_cache_append; also ERR_SHAPE for a scale or softcap that is negative or not finite, O the same buffer as Q, or a
  * plan that is not this call's, ERR_CAPACITY for a workspace that is too small. */

@@ -9,10 +9,12 @@
 // The blocks' scales are powers of two: those of the keys go into the factor between scores and the exponential, those of the values
 // into the exponent of the weights.
 //
-// A row's reference M is lazy: weights are 2^(z - M + LIFT) in f16, whose range bears scores ABOVE over M, so sums are rescaled only where a
-// page's largest score exceeds M by more than that (many rows: where the weights' sum says that one may), or where a block's
-// values have a larger scale than all before.
-// Weights keep their 11 bits down to 2^-23 of M's, so thousands of keys that share what one strong key leaves are held.
+// What a key gives to a row is its weight times its block's scale 2^e, so a row's references are two: M for z and V for the scales, with M + V for z + e.
+// Weights are 2^(z + e - M - V + LIFT) in f16, and all that a row sees counts by what it gives: a block that is hidden from the row or has no
+// weight takes no bits from the others, however large its values are.  (With the largest e of the pages read in place of V it would.)  The
+// references are lazy: f16 bears ABOVE over them, so sums are rescaled only where z or z + e exceeds its reference by more than that
+// (many rows: where the weights' sum says that one may).  Weights keep their 11 bits down to 2^-23 of M + V, so thousands of keys that share
+// what one strong key leaves are held.  The weights' own sum, without scales, is fp32's, relative to M.
 //
 // Both products are written transposed, so that what the first leaves in a lane is what the second wants there:
 //   S^T = K Q^T   A = keys x dims, B = dims x rows;   O^T = V^T P^T   A = dims x tokens, B = tokens x rows
@@ -119,31 +121,37 @@ __device__ __forceinline__ work_item find_work(const epara_cache_attn_args* __re
     return w;
 }
 
-// 8 bytes that a workgroup on another die has written or will read in this kernel: past the dies' own caches.
-__device__ __forceinline__ void put2(float* at, float a, float b)
-{
-    __hip_atomic_store(reinterpret_cast<unsigned long long*>(at), (static_cast<unsigned long long>(__float_as_uint(b)) << 32) | __float_as_uint(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
+// 8 bytes that a workgroup on another die has written in this kernel: past the dies' own caches.  (Each lane of its own slot: a buffer's descriptor would have to be
+// the same for all lanes.)
 __device__ __forceinline__ v2f get2(const float* at)
 {
     const unsigned long long v = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     return v2f{__uint_as_float(static_cast<uint32_t>(v)), __uint_as_float(static_cast<uint32_t>(v >> 32))};
 }
 
-template <bool V> struct flag { static constexpr bool value = V; };
 constexpr float NOTHING = -1e30f;                          // reference of a row that has seen no key
 constexpr float ABOVE = 6.f, LIFT = 9.f;                   // a weight is at most 2^(ABOVE + LIFT) = 2^15
 constexpr float MOST = 32768.f;                            // sum of weights in which none can be more than that
+constexpr float FAR = 4000.f;                              // farther than any two scales
+constexpr int NO_SCALE = -1000;                            // the values' reference before any page
+constexpr int LEAST_SHIFT = -60;                           // of a block's scale under V: such weights are zeros in f16, their sum still is fp32's
 
-struct row_state { float ref, sum; };                      // M, and the sum of the weights relative to it (of this lane's keys)
+struct row_state { float ref; int scale; float sum; };     // M, V, and the sum of the weights relative to M (of this lane's keys)
 
-// What turns sums relative to s.ref into sums relative to the page's largest score `top` (units of log 2; -inf: the row sees none of it), which
-// is s.ref from then on.
-__device__ __forceinline__ float raise_reference(row_state& s, float top)
+// Makes the references those of what has been and of a page, and gives the factor for sums of weights times values.  top: the row's largest score
+// of the page in units of log 2 (-inf: the row sees none of it); mine: of this lane's keys, whose block's scale is 2^exponent; LANES:
+// distances of the lanes that hold the others.
+template <int... LANES>
+__device__ __forceinline__ float raise_references(row_state& s, float top, float mine, int exponent)
 {
-    const float to = top > s.ref ? __builtin_ceilf(top) : s.ref, f = __builtin_amdgcn_exp2f(s.ref - to);
+    const float to = top > s.ref ? __builtin_ceilf(top) : s.ref, gone = s.ref - to;
+    int scale = static_cast<int>(__builtin_ceilf(fmaxf(mine - to, -FAR))) + exponent;
+    ((scale = max_of(scale, __shfl_xor(scale, LANES))), ...);
+    scale = max_of(scale, s.scale + static_cast<int>(fmaxf(gone, -FAR)));
+    const float f = __builtin_amdgcn_exp2f(gone + static_cast<float>(s.scale - scale));
     s.ref = to;
-    s.sum *= f;
+    s.scale = scale;
+    s.sum *= __builtin_amdgcn_exp2f(gone);
     return f;
 }
 
@@ -158,8 +166,6 @@ __device__ __forceinline__ page_scales scales_of(uint32_t word, bool second_bloc
     s.value[1] = second_block ? static_cast<int>(word >> 24) - 127 : s.value[0];
     return s;
 }
-constexpr int NO_SCALE = -1000;                            // the values' reference before any page
-constexpr int LEAST_SHIFT = -60;                           // values under 2^-60 of the largest: their weights are zeros in f16, their sum still is fp32's
 
 __device__ __forceinline__ float capped_score(float z, float in, float out)      // c tanh(z / c) = c (1 - 2 / (1 + e^(2 z / c))), in units of log 2
 {
@@ -197,8 +203,9 @@ struct few_lds {
         float o[WAVES][FEW_TILE][D + 4];                   // a part: the waves' sums
         v4f joined[WAVES][FEW_TILE * D / 4];               // joining the parts: the waves' sums again
     };
-    float m[WAVES][FEW_TILE], l[WAVES][FEW_TILE];
+    float m[WAVES][FEW_TILE], l[WAVES][FEW_TILE], v[WAVES][FEW_TILE];
     float weight[MAX_PARTS][FEW_TILE];                     // of a part's sums in the result
+    int scale[FEW_TILE];                                   // of the rows' results
     uint32_t last;
 };
 
@@ -210,6 +217,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t slot_of(char* slots, size_t it
 __device__ __forceinline__ void put4(__amdgpu_buffer_rsrc_t slot, int at, v4f x) { __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4i, x), slot, at, 0, 16); }
 __device__ __forceinline__ v4f get4(__amdgpu_buffer_rsrc_t slot, int at) { return __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(slot, at, 0, 16)); }
 
+__device__ __forceinline__ v4f scaled4(v4f x, int e) { return v4f{__builtin_ldexpf(x[0], e), __builtin_ldexpf(x[1], e), __builtin_ldexpf(x[2], e), __builtin_ldexpf(x[3], e)}; }
+
 // Four consecutive columns of an output row of a tile of `size` rows.
 __device__ __forceinline__ void store_out4(const work_item& w, int row, int col, v4f x)
 {
@@ -218,47 +227,16 @@ __device__ __forceinline__ void store_out4(const work_item& w, int row, int col,
     *reinterpret_cast<EPARA_GLOBAL v2u*>(dst) = v2u{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
 }
 
-// A slot of few rows: 16 rows of D sums, then 16 pairs (reference, sum of weights).
+// Sums that several waves or parts have of a row are of references (M, V) of their own.  They are added relative to the largest M and the largest
+// V + M - that M, and get their scale once they have been divided by the sum of weights: before, they may leave fp32's range.
+
+// A slot of few rows: 16 rows of D sums, then 16 x (M, sum of weights, V).
 constexpr int FEW_SLOT = FEW_TILE * SLOT_FLOATS * 4;
 
-// All parts of a tile are in their slots: their weighted sum, in the order of the parts inside a wave and of the waves, so the same bits every time.
-template <int D>
-__device__ __forceinline__ void join_few(const work_item& w, char* slots, few_lds<D>& lds, int wave, int lane)
+// A wave's share of the parts: the first STEPS * 64 pieces of 16 bytes of each.  No branch lies between the loads, so those of several parts are in flight.
+template <int D, int STEPS>
+__device__ __forceinline__ void add_parts(const work_item& w, char* slots, few_lds<D>& lds, int wave, int lane)
 {
-    const int tid = wave * 64 + lane, rows = min_of(FEW_TILE, w.rows - w.tile * FEW_TILE);
-    {   // thread = (row, one of 16): weights of the parts.  A row that sees no key: zeros
-        const int r = tid >> 4, j = tid & 15;
-        float ref[MAX_PARTS / 16], sum[MAX_PARTS / 16], top = NOTHING;
-#pragma unroll
-        for (int i = 0; i < MAX_PARTS / 16; ++i) {
-            ref[i] = NOTHING;
-            sum[i] = 0.f;
-            if (j + 16 * i < w.parts && r < rows) {
-                const v2f ml = get2(reinterpret_cast<const float*>(slots + (w.first_item + static_cast<size_t>(j + 16 * i) * w.stride) * FEW_SLOT) + FEW_TILE * D + 2 * r);
-                ref[i] = ml[0];
-                sum[i] = ml[1];
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < MAX_PARTS / 16; ++i) top = fmaxf(top, ref[i]);
-#pragma unroll
-        for (int d = 8; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-        float total = 0.f;
-#pragma unroll
-        for (int i = 0; i < MAX_PARTS / 16; ++i) {
-            ref[i] = __builtin_amdgcn_exp2f(ref[i] - top);
-            total += sum[i] * ref[i];
-        }
-#pragma unroll
-        for (int d = 8; d >= 1; d >>= 1) total += __shfl_xor(total, d);
-        const float inv = top == NOTHING ? 0.f : 1.f / total;
-#pragma unroll
-        for (int i = 0; i < MAX_PARTS / 16; ++i)
-            if (j + 16 * i < w.parts) lds.weight[j + 16 * i][r] = ref[i] * inv;
-    }
-    __syncthreads();
-    constexpr int STEPS = FEW_TILE * D / 256;              // 16-byte pieces of a slot per lane
-    const int pieces = rows * D / 4;
     v4f acc[STEPS];
 #pragma unroll
     for (int k = 0; k < STEPS; ++k) acc[k] = v4f{0.f, 0.f, 0.f, 0.f};
@@ -267,18 +245,72 @@ __device__ __forceinline__ void join_few(const work_item& w, char* slots, few_ld
         const __amdgpu_buffer_rsrc_t slot = slot_of(slots, w.first_item + static_cast<size_t>(i) * w.stride, FEW_SLOT);
 #pragma unroll
         for (int k = 0; k < STEPS; ++k) {
-            if (k * 64 >= pieces) break;
             const int e = lane + 64 * k;                   // a piece past the rows reads what the slot holds, and is not stored
             acc[k] += get4(slot, e * 16) * lds.weight[i][e / (D / 4)];
         }
     }
 #pragma unroll
     for (int k = 0; k < STEPS; ++k) lds.joined[wave][lane + 64 * k] = acc[k];
+}
+
+// All parts of a tile are in their slots: their weighted sum, in the order of the parts inside a wave and of the waves, so the same bits every time.
+template <int D>
+__device__ __forceinline__ void join_few(const work_item& w, char* slots, few_lds<D>& lds, int wave, int lane)
+{
+    const int tid = wave * 64 + lane, rows = min_of(FEW_TILE, w.rows - w.tile * FEW_TILE);
+    {   // thread = (row, one of 16): weights of the parts.  A row that sees no key: zeros
+        const int r = tid >> 4, j = tid & 15;
+        float ref[MAX_PARTS / 16], sum[MAX_PARTS / 16], scale[MAX_PARTS / 16], top = NOTHING;
+        v2f in[MAX_PARTS / 16][2];
+#pragma unroll
+        for (int i = 0; i < MAX_PARTS / 16; ++i) {         // (a part or row that is not there: what another one's place holds)
+            if (16 * i >= w.parts) break;
+            const float* s = reinterpret_cast<const float*>(slots + (w.first_item + static_cast<size_t>(min_of(j + 16 * i, w.parts - 1)) * w.stride) * FEW_SLOT) + FEW_TILE * D + 4 * r;
+            in[i][0] = get2(s);
+            in[i][1] = get2(s + 2);
+        }
+#pragma unroll
+        for (int i = 0; i < MAX_PARTS / 16; ++i) {
+            const bool there = j + 16 * i < w.parts && r < rows;
+            ref[i] = there ? in[i][0][0] : NOTHING;
+            sum[i] = there ? in[i][0][1] : 0.f;
+            scale[i] = there ? in[i][1][0] : NO_SCALE;
+        }
+#pragma unroll
+        for (int i = 0; i < MAX_PARTS / 16; ++i) top = fmaxf(top, ref[i]);
+#pragma unroll
+        for (int d = 8; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+        float total = 0.f, widest = NO_SCALE;
+#pragma unroll
+        for (int i = 0; i < MAX_PARTS / 16; ++i) {
+            total += sum[i] * __builtin_amdgcn_exp2f(ref[i] - top);
+            scale[i] += ref[i] - top;
+            widest = fmaxf(widest, scale[i]);
+        }
+#pragma unroll
+        for (int d = 8; d >= 1; d >>= 1) {
+            total += __shfl_xor(total, d);
+            widest = fmaxf(widest, __shfl_xor(widest, d));
+        }
+        const float inv = top == NOTHING ? 0.f : 1.f / total;
+#pragma unroll
+        for (int i = 0; i < MAX_PARTS / 16; ++i)
+            if (j + 16 * i < w.parts) lds.weight[j + 16 * i][r] = __builtin_amdgcn_exp2f(scale[i] - widest) * inv;
+        if (j == 0) lds.scale[r] = static_cast<int>(widest);
+    }
+    __syncthreads();
+    constexpr int STEPS = FEW_TILE * D / 256;              // 16-byte pieces of a slot per lane
+    const int pieces = rows * D / 4;
+    if (pieces <= 64)                  add_parts<D, 1>(w, slots, lds, wave, lane);
+    else if (pieces <= 128)            add_parts<D, 2>(w, slots, lds, wave, lane);
+    else if (STEPS == 4 || pieces <= 256) add_parts<D, 4>(w, slots, lds, wave, lane);
+    else                               add_parts<D, STEPS>(w, slots, lds, wave, lane);
     __syncthreads();
     for (int e = tid; e < pieces; e += NT) {
         v4f x = lds.joined[0][e];
 #pragma unroll
         for (int i = 1; i < WAVES; ++i) x += lds.joined[i][e];
+        x = scaled4(x, lds.scale[e / (D / 4)]);
         store_out4(w, w.tile * FEW_TILE + e / (D / 4), e % (D / 4) * 4, x);
     }
 }
@@ -339,8 +371,7 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
     };
     page_list list = pages_of(w, pages, lane);
 
-    row_state state = {NOTHING, 0.f};
-    int v_ref = NO_SCALE;
+    row_state state = {NOTHING, NO_SCALE, 0.f};
     v4f o[D / 16];
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) o[d] = v4f{0.f, 0.f, 0.f, 0.f};
@@ -396,23 +427,22 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
                 }
             unit = 1.f;
         }
-        // ---- the row's largest score here: mine are 16 keys of the page, the lanes n, n + 16, .. hold the others
-        float top = -INFINITY;
+        // ---- the row's largest score here: mine are 16 keys of one block, the lanes n, n + 16, .. hold the others
+        float mine = -INFINITY;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) top = fmaxf(top, fmaxf(fmaxf(z[t][0], z[t][1]), fmaxf(z[t][2], z[t][3])));
-        top *= unit;
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const int v_top = max_of(ps.value[0], ps.value[1]);
-        if (__ballot(top > state.ref + ABOVE || v_top > v_ref)) {
-            const int to = max_of(v_ref, v_top);
-            const float f = raise_reference(state, top) * __builtin_amdgcn_exp2f(static_cast<float>(v_ref - to));
-            v_ref = to;
+        for (int t = 0; t < 4; ++t) mine = fmaxf(mine, fmaxf(fmaxf(z[t][0], z[t][1]), fmaxf(z[t][2], z[t][3])));
+        mine *= unit;
+        const int exponent = q < 2 ? ps.value[0] : ps.value[1];
+        const float over = mine - state.ref;
+        if (__ballot(over > ABOVE || over + static_cast<float>(exponent - state.scale) > ABOVE)) {
+            float top = fmaxf(mine, __shfl_xor(mine, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float f = raise_references<16, 32>(state, top, mine, exponent);
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) o[d] *= f;
         }
-        const int v_shift = max_of((q < 2 ? ps.value[0] : ps.value[1]) - v_ref, LEAST_SHIFT);      // <= 0: my values' block against the largest so far
-        const float lift = LIFT - state.ref + static_cast<float>(v_shift);
+        const int shift = max_of(exponent - state.scale, LEAST_SHIFT);      // my block's scale against V
+        const float lift = LIFT - state.ref + static_cast<float>(shift);
         float sum = 0.f, weight[16];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -421,7 +451,7 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
                 weight[4 * t + i] = __builtin_amdgcn_exp2f(fmaf(z[t][i], unit, lift));
                 sum += weight[4 * t + i];
             }
-        state.sum += sum * exp2_int(-v_shift);
+        state.sum += __builtin_ldexpf(sum, -shift);
         const v8h w0 = narrow(weight), w1 = narrow(weight + 8);
         // ---- values.  What lies behind the last token may be anything, a NaN too: cleared
         if (p * PAGE + PAGE > end) {
@@ -445,29 +475,28 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
     state.sum += __shfl_xor(state.sum, 16);
     state.sum += __shfl_xor(state.sum, 32);
 
-    const float v_unit = v_ref == NO_SCALE ? 0.f : exp2_int(v_ref);
-#pragma unroll
-    for (int d = 0; d < D / 16; ++d) o[d] *= v_unit;
-
     // ---- the four waves' sums: thread = (row, D / 16 columns)
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) *reinterpret_cast<v4f*>(&lds.o[wave][n][d * 16 + q * 4]) = o[d];
     if (q == 0) {
         lds.m[wave][n] = state.ref;
         lds.l[wave][n] = state.sum;
+        lds.v[wave][n] = static_cast<float>(state.scale);
     }
     __syncthreads();
     constexpr int COLS = D / 16;
     const int r = tid >> 4, c = (tid & 15) * COLS;
-    float mm = NOTHING, ll = 0.f, oo[COLS];
+    float mm = NOTHING, ll = 0.f, vv = NO_SCALE, oo[COLS];
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) mm = fmaxf(mm, lds.m[i][r]);
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) vv = fmaxf(vv, lds.v[i][r] + (lds.m[i][r] - mm));
 #pragma unroll
     for (int j = 0; j < COLS; ++j) oo[j] = 0.f;
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) {
-        const float weight = __builtin_amdgcn_exp2f(lds.m[i][r] - mm);
-        ll += weight * lds.l[i][r];
+        const float over = lds.m[i][r] - mm, weight = __builtin_amdgcn_exp2f(lds.v[i][r] + over - vv);
+        ll += __builtin_amdgcn_exp2f(over) * lds.l[i][r];
 #pragma unroll
         for (int j = 0; j < COLS; ++j) oo[j] += weight * lds.o[i][r][c + j];
     }
@@ -477,7 +506,7 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
         if (out_row < w.rows) {
 #pragma unroll
             for (int j = 0; j < COLS; j += 4) put4(slot, (r * D + c + j) * 4, v4f{oo[j], oo[j + 1], oo[j + 2], oo[j + 3]});
-            if (c == 0) put2(reinterpret_cast<float*>(slots + static_cast<size_t>(item) * FEW_SLOT) + FEW_TILE * D + 2 * r, mm, ll);
+            if (c == 0) put4(slot, (FEW_TILE * D + 4 * r) * 4, v4f{mm, ll, vv, 0.f});
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
@@ -491,7 +520,7 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
     if (out_row >= w.rows) return;
     const float inv = mm == NOTHING ? 0.f : 1.f / ll;      // a row that sees no key: zeros
 #pragma unroll
-    for (int j = 0; j < COLS; j += 4) store_out4(w, out_row, c + j, v4f{oo[j], oo[j + 1], oo[j + 2], oo[j + 3]} * inv);
+    for (int j = 0; j < COLS; j += 4) store_out4(w, out_row, c + j, scaled4(v4f{oo[j], oo[j + 1], oo[j + 2], oo[j + 3]} * inv, static_cast<int>(vv)));
 }
 
 __global__ __launch_bounds__(NT, 2) void attend_few_kernel(const epara_cache_attn_args* __restrict__ args, const epara_sequence* __restrict__ seqs,
@@ -588,8 +617,7 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
         }
     };
 
-    row_state state = {NOTHING, 0.f};
-    int v_ref = NO_SCALE;
+    row_state state = {NOTHING, NO_SCALE, 0.f};
     v16f o[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -671,17 +699,12 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d] *= f;
         };
-        const int v_top = max_of(ps.value[0], ps.value[1]);
-        if (v_top > v_ref) {
-            scale_sums(__builtin_amdgcn_exp2f(static_cast<float>(v_ref - v_top)));
-            v_ref = v_top;
-        }
-        // ---- weights of a tile, and their sum without the values' scale (in fp32 before they are rounded: a block of small values may leave f16 nothing of
-        // its weights, but the sum needs them).  The reference is raised only where the sum says that a weight may have left f16's range: no
+        // ---- weights of a tile, and their sum with and without (`plain`) the values' scale (in fp32 before they are rounded: a block of small values may leave f16
+        // nothing of its weights, but the sum needs them).  The references are raised only where the sum says that a weight may have left f16's range: no
         // maximum is formed otherwise.  The first page's weights are infinite against NOTHING.
-        auto weigh = [&](int u, v8h* weights) -> float {
-            const int v_shift = max_of(ps.value[u] - v_ref, LEAST_SHIFT);       // <= 0
-            const float lift = LIFT - state.ref + static_cast<float>(v_shift);
+        auto weigh = [&](int u, v8h* weights, float& plain) -> float {
+            const int shift = max_of(ps.value[u] - state.scale, LEAST_SHIFT);
+            const float lift = LIFT - state.ref + static_cast<float>(shift);
             float x[16], sum[2] = {0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -690,7 +713,8 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
             }
             weights[0] = narrow(x);
             weights[1] = narrow(x + 8);
-            return (sum[0] + sum[1]) * exp2_int(-v_shift);
+            plain = __builtin_ldexpf(sum[0] + sum[1], -shift);
+            return sum[0] + sum[1];
         };
         auto raise = [&](int u) {
             float top = z[u][0];
@@ -698,7 +722,7 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
             for (int i = 1; i < 16; ++i) top = fmaxf(top, z[u][i]);
             top *= unit[u];
             top = fmaxf(top, __shfl_xor(top, 32));         // the other half of the row
-            scale_sums(raise_reference(state, top));
+            scale_sums(raise_references<>(state, top, top, ps.value[u]));
         };
         auto add_values = [&](int u, const v8h* weights) {
 #pragma unroll
@@ -708,44 +732,39 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
                     o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds8h(here + VALUES + ((d * 2 + u) * 2 + j) * 1024), weights[j], o[d], 0, 0, 0);
         };
         v8h first[2], second[2];
-        float sum = weigh(0, first);
-        if (__ballot(sum > MOST)) {
+        float plain;
+        if (__ballot(weigh(0, first, plain) > MOST)) {
             raise(0);
-            sum = weigh(0, first);
+            weigh(0, first, plain);
         }
-        state.sum += sum;
+        state.sum += plain;
         add_values(0, first);
-        sum = weigh(1, second);
-        if (__ballot(sum > MOST)) {
+        if (__ballot(weigh(1, second, plain) > MOST)) {
             raise(1);
-            sum = weigh(1, second);
+            weigh(1, second, plain);
         }
-        state.sum += sum;
+        state.sum += plain;
         add_values(1, second);
         swap();
         next = later;
     }
     only_bring(w.hi);
-    const float v_unit = v_ref == NO_SCALE ? 0.f : exp2_int(v_ref);
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] *= v_unit;
     state.sum += __shfl_xor(state.sum, 32);
 
+    float scale = static_cast<float>(state.scale);
     if (w.parts > 1) {
-        // a slot: per wave 1 KiB for each quad of registers, then the references and sums
+        // a slot: per wave 1 KiB for each quad of registers, then 32 x (M, sum of weights, V)
         char* slot_at = slots + static_cast<size_t>(item) * MANY_TILE * SLOT_FLOATS * 4;
         __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(slot_at, 0, MANY_TILE * SLOT_FLOATS * 4, 0x00020000);
         constexpr int WAVE_BYTES = 32 * SLOT_FLOATS * 4;
-        const int at = wave * WAVE_BYTES + lane * 16;
+        const int at = wave * WAVE_BYTES + lane * 16, refs_at = wave * WAVE_BYTES + 16384 + n * 16;
         if (live) {
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4i, v4f{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]}), rsrc, at, (d * 4 + j) * 1024, 16);   // 16: device scope
-            if (h == 0) put2(reinterpret_cast<float*>(slot_at + wave * WAVE_BYTES + 16384) + 2 * n, state.ref, state.sum);
+            if (h == 0) put4(rsrc, refs_at, v4f{state.ref, state.sum, scale, 0.f});
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
@@ -755,7 +774,8 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
         if (*box != static_cast<uint32_t>(w.parts - 1)) return;
         if (tid == 0) __hip_atomic_store(counters + w.first_item, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         if (!live) return;
-        state = {NOTHING, 0.f};
+        state = {NOTHING, NO_SCALE, 0.f};
+        scale = NO_SCALE;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -763,15 +783,17 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
         for (int i = 0; i < w.parts; ++i) {
             char* from = slots + (static_cast<size_t>(w.first_item) + static_cast<size_t>(i) * w.stride) * MANY_TILE * SLOT_FLOATS * 4;
             rsrc = __builtin_amdgcn_make_buffer_rsrc(from, 0, MANY_TILE * SLOT_FLOATS * 4, 0x00020000);
-            const v2f ml = get2(reinterpret_cast<const float*>(from + wave * WAVE_BYTES + 16384) + 2 * n);
+            const v4f s = get4(rsrc, refs_at);
             v4i in[DT][4];
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) in[d][j] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, (d * 4 + j) * 1024, 16);
-            const float both = fmaxf(state.ref, ml[0]), keep = __builtin_amdgcn_exp2f(state.ref - both), add = __builtin_amdgcn_exp2f(ml[0] - both);
+            const float both = fmaxf(state.ref, s[0]), gone = state.ref - both, over = s[0] - both, wider = fmaxf(scale + gone, s[2] + over);
+            const float keep = __builtin_amdgcn_exp2f(scale + gone - wider), add = __builtin_amdgcn_exp2f(s[2] + over - wider);
             state.ref = both;
-            state.sum = state.sum * keep + ml[1] * add;
+            state.sum = state.sum * __builtin_amdgcn_exp2f(gone) + s[1] * __builtin_amdgcn_exp2f(over);
+            scale = wider;
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -785,6 +807,7 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
     if (!live) return;
     // ---- rows out.  Lane (n, h) holds dims 32 d + 8 j + 4 h + 0 .. 3; two quads change places between the halves of the wave, so that a lane stores 8 in a row
     const float inv = state.ref == NOTHING ? 0.f : 1.f / state.sum;
+    const int unit = static_cast<int>(scale);
     const bool mine = first_row + n < w.rows;
     EPARA_GLOBAL char* dst = (EPARA_GLOBAL char*)a.O + (static_cast<size_t>(w.s.first_row + token) * a.o_stride + static_cast<size_t>(query_head) * D) * 2;
 #pragma unroll
@@ -794,7 +817,9 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
             v4i out;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const uint32_t x = pack_bf16(o[d][4 * j + 2 * e] * inv, o[d][4 * j + 2 * e + 1] * inv), y = pack_bf16(o[d][4 * j + 4 + 2 * e] * inv, o[d][4 * j + 5 + 2 * e] * inv);
+                const int a = 4 * j + 2 * e, b = a + 4;
+                const uint32_t x = pack_bf16(__builtin_ldexpf(o[d][a] * inv, unit), __builtin_ldexpf(o[d][a + 1] * inv, unit));
+                const uint32_t y = pack_bf16(__builtin_ldexpf(o[d][b] * inv, unit), __builtin_ldexpf(o[d][b + 1] * inv, unit));
                 const v2u both = __builtin_bit_cast(v2u, __builtin_amdgcn_permlane32_swap(x, y, false, false));
                 out[e] = static_cast<int>(both[0]);
                 out[2 + e] = static_cast<int>(both[1]);

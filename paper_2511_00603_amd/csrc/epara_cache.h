@@ -54,7 +54,7 @@ constexpr int FEW_TILE = 16, MANY_TILE = 128;
 // waves idle: 2 requests with 32 rows at 8000 tokens 16 us against 34, 16 of them 59 against 56; 64 rows 21 against 38 and 118 against 71.
 constexpr int FEW_MAX_ROWS = 32;
 constexpr int MAX_PARTS = 128;                             // of a tile's pages
-constexpr int SLOT_FLOATS = 128 + 2;                       // per row of a part: the weighted sum of values, maximum, sum of weights
+constexpr int SLOT_FLOATS = 128 + 4;                       // per row of a part: the weighted sum of values, both references and the sum of weights
 EPARA_BOTH bool has_few_rows(const epara_cache_attn_args& a, const epara_sequence& s) { return static_cast<int64_t>(s.rows) * (a.heads / a.kv_heads) <= FEW_MAX_ROWS; }
 
 struct page_range { int lo, hi; };

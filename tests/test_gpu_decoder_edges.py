@@ -1,0 +1,86 @@
+"""GPU parity of a decoder block's pieces where their inputs are far from ordinary, against oracle/decoder.py in 64 bits on the same bits.  Tolerances are those of
+test_gpu_decoder.py, which derives them."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import decoder as OD
+from paper_2511_00603_amd import runtime as R
+from test_gpu_decoder import BF, DEV, Case, check_attn, dev_bf16, fetch, run_attn, sync
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- attention ---------------------------------------------------------------------------------------------------
+
+def one_sequence(rng, n, rows, D, K, V, q, window=0, softcap=0.0, group=2):
+    """The last `rows` of n tokens K, V [n, 1, D] with the queries q [rows, group * D], ready for run_attn and check_attn."""
+    case = Case(rng, [n], group, 1, D)
+    case.oracle.append(case.pages[0], 0, K, V)
+    case.upload()
+    q, Q = dev_bf16(q)
+    O = torch.zeros(rows, group * D, dtype=torch.bfloat16, device=DEV)
+    return (case, [{"first_row": 0, "rows": rows, "start": n - rows, "pages": case.pages[0]}],
+            {"Q": Q, "O": O, "cache": case.cache, "heads": group, "window": window, "softcap": softcap}, q.reshape(rows, group, D))
+
+
+@pytest.mark.parametrize("rows", [1, 3, 16, 90, 200])
+@pytest.mark.parametrize("huge", [1e6, 1e10, 1e30])
+def test_attention_of_rows_that_do_not_see_a_block_of_huge_values(rows, huge):
+    """Blocks of huge values behind a row, or left by its window, take nothing from it: few and many rows, rows on both sides in one tile."""
+    for D in (64, 128):
+        for lo, hi, window in ((224, 256, 0), (288, 300, 0), (32, 64, 0), (0, 32, 37), (96, 128, 70), (224, 256, 20)):
+            n, rng = 300, np.random.default_rng([101, rows, D, lo])
+            K, V = rng.standard_normal((n, 1, D)), rng.standard_normal((n, 1, D))
+            V[lo:hi] *= huge
+            c = one_sequence(rng, n, rows, D, K, V, rng.standard_normal((rows, 2 * D)), window)
+            run_attn([c])
+            check_attn([c])
+
+
+@pytest.mark.parametrize("rows", [1, 3, 90])
+@pytest.mark.parametrize("huge", [1e-20, 1e-6, 1e6, 1e10, 1e30])
+def test_attention_of_blocks_of_huge_values_with_next_to_no_weight(rows, huge):
+    """What a block gives is its weight times its values: huge values whose weights are e^-60 and less of the others' take no bits from small ones that have all the weight, and
+    tiny values of strong keys leave the others theirs; one order and the other."""
+    for D in (64, 128):
+        for lo, hi in ((0, 32), (128, 192), (256, 288)):
+            n, rng = 330, np.random.default_rng([102, rows, D, lo])
+            K, V = rng.standard_normal((n, 1, D)) * 0.3, rng.standard_normal((n, 1, D))
+            V[lo:hi] *= huge
+            K[:, 0, 0] = 2.0
+            K[lo:hi, 0, 0] = 2.0 - (np.log(huge) + 60.0) / 4.0 if huge > 1 else 6.0
+            q = rng.standard_normal((rows, 2 * D))
+            q[:, 0] = q[:, D] = 4.0 * D ** 0.5
+            c = one_sequence(rng, n, rows, D, K, V, q)
+            run_attn([c])
+            check_attn([c])
+
+
+@pytest.mark.parametrize("rows", [1, 40, 100])
+def test_attention_joins_parts_of_very_different_values(rows):
+    """Parts of a long context, each of one magnitude of values (of whole blocks), from 2^-60 to 2^99 in any order, the largest with the least weight: all of them give alike."""
+    n, D = 6 * 1024, 64
+    rng = np.random.default_rng([105, rows])
+    K, V = rng.standard_normal((n, 1, D)) * 0.2, rng.standard_normal((n, 1, D))
+    level = np.repeat(rng.integers(-60, 100, 6), 1024)
+    V *= np.exp2(level)[:, None, None]
+    K[:, 0, 0] = -level * np.log(2.0) / 4.0 + rng.standard_normal(n) * 0.1
+    q = rng.standard_normal((rows, D))
+    q[:, 0] = 4.0 * D ** 0.5
+    c = one_sequence(rng, n, rows, D, K, V, q, group=1)
+    plan = run_attn([c])
+    assert plan.plan.workspace_bytes > 0
+    check_attn([c])
+
+
+@pytest.mark.parametrize("rows", [1, 90])
+def test_attention_of_values_at_the_end_of_the_range(rows):
+    """Means of values near bf16's largest are finite as those values are."""
+    for D in (64, 128):
+        n, rng = 200, np.random.default_rng([104, rows, D])
+        K, V = rng.standard_normal((n, 1, D)) * 0.1, np.full((n, 1, D), 3.2e38) * np.sign(rng.standard_normal(D))
+        V[40:80] *= 0.25
+        c = one_sequence(rng, n, rows, D, K, V, rng.standard_normal((rows, 2 * D)))
+        run_attn([c])
+        check_attn([c])
