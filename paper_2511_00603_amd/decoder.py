@@ -69,17 +69,61 @@ class DecoderBlock:
     # ---- one step
     def step(self, new):
         """new: per service a list of (sequence name, X [tokens, d] bf16 on the GPU) -> per service a dict of the step's tensors, rows in the order of the list.  A name that
-        is not known yet begins a sequence."""
+        is not known yet begins a sequence.  A step that raises leaves all sequences and pages as they were: EparaError (ERR_CAPACITY) where a service has too few
+        free pages, ValueError for a name twice, tokens of another shape, or more positions than the table of angles has."""
+        work = self._admit(new)
+        try:
+            tensors = self._launch(new, work)
+        except BaseException:
+            self._give_back(work)
+            raise
+        self._commit(work)
+        return tensors
+
+    def _admit(self, new):
+        """-> per service a list of (name, position of the first new token, tokens, pages with the new ones, the new ones): checked, and the pages taken; no sequence is
+        changed yet."""
+        if len(new) != len(self.params):
+            raise ValueError("%d services, tokens for %d" % (len(self.params), len(new)))
+        work, limit = [], int(self.rotary.shape[0])
+        for g, (items, p) in enumerate(zip(new, self.params)):
+            if len({name for name, _ in items}) != len(items):
+                raise ValueError("a sequence is named twice in one step")
+            for name, X in items:
+                if X.dim() != 2 or X.shape[1] != p.Wqkv.shape[0] or X.dtype != torch.bfloat16:
+                    raise ValueError("sequence %r: tokens are bfloat16 [n, %d]" % (name, p.Wqkv.shape[0]))
+                if self.sequences[g].get(name, [[], 0])[1] + int(X.shape[0]) > limit:
+                    raise ValueError("sequence %r: more than %d positions" % (name, limit))
+        try:
+            for g, items in enumerate(new):
+                work.append([])
+                for name, X in items:
+                    pages, start = self.sequences[g].get(name, [[], 0])
+                    n = int(X.shape[0])
+                    fresh = self.pools[g].take(max(0, -(-(start + n) // B.EPARA_CACHE_PAGE) - len(pages))).tolist()
+                    work[g].append((name, start, n, pages + fresh, fresh))
+        except BaseException:
+            self._give_back(work)
+            raise
+        return work
+
+    def _give_back(self, work):
+        for g, items in enumerate(work):
+            for _, _, _, _, fresh in reversed(items):
+                self.pools[g].free(fresh[::-1])
+
+    def _commit(self, work):
+        for g, items in enumerate(work):
+            for name, start, n, pages, _ in items:
+                self.sequences[g][name] = [pages, start + n]
+
+    def _launch(self, new, work):
         dev, bf = self.device, B.EPARA_BF16
         table, tensors = [], []
         for g, (items, p) in enumerate(zip(new, self.params)):
             seqs, row = [], 0
-            for name, X in items:
-                seq = self.sequences[g].setdefault(name, [[], 0])
-                n = int(X.shape[0])
-                seq[0] += self.pools[g].take(max(0, -(-(seq[1] + n) // B.EPARA_CACHE_PAGE) - len(seq[0]))).tolist()
-                seqs.append({"first_row": row, "rows": n, "start": seq[1], "pages": seq[0]})
-                seq[1] += n
+            for _, start, n, pages, _ in work[g]:
+                seqs.append({"first_row": row, "rows": n, "start": start, "pages": pages})
                 row += n
             table.append(seqs)
             d, width = p.Wqkv.shape
