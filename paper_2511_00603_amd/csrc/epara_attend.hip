@@ -167,9 +167,27 @@ __device__ __forceinline__ page_scales scales_of(uint32_t word, bool second_bloc
     return s;
 }
 
-__device__ __forceinline__ float capped_score(float z, float in, float out)      // c tanh(z / c) = c (1 - 2 / (1 + e^(2 z / c))), in units of log 2
+// A service's cap, c: in units of log 2 a score is c tanh(z / c) = c (1 - 2 / (1 + e^(2 z / c))), whose error is c's share of fp32's, some 2e-7 c: 1e-4 at
+// WIDE.  Above, scores far under c are taken from the series of tanh, which keeps their own bits.  A cap beyond LARGEST changes no score that
+// fp32 could tell from another; one under LEAST makes all weights of a sign 1, as LEAST does.
+struct score_cap {
+    static constexpr float WIDE = 512.f, LARGEST = 0x1p64f, LEAST = 0x1p-64f;
+    bool on, wide;
+    float in, out;                                         // of a score in units of the query's head: to 2 z / (c log 2), and c / log 2
+};
+__device__ __forceinline__ score_cap cap_of(const epara_cache_attn_args& a, float q_unit)
 {
-    return out - 2.f * out * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * in));
+    const float c = fmaxf(a.softcap, score_cap::LEAST);
+    const bool on = a.softcap > 0.f && a.softcap < score_cap::LARGEST;
+    return {on, on && c > score_cap::WIDE, (on ? 2.f * LOG2E * a.scale / c : a.scale * LOG2E) * q_unit, c * LOG2E};
+}
+__device__ __forceinline__ float capped_score(float z, float in, float out) { return out - 2.f * out * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * in)); }
+// tanh u = u - u^3 / 3 + 2 u^5 / 15 - 17 u^7 / 315 + 62 u^9 / 2835 - ..: what is left out is under 1e-8 of it at 1 / 4.
+__device__ __forceinline__ float widely_capped_score(float z, float in, float out)
+{
+    const float u = z * in * (0.5f / LOG2E), s = u * u;
+    const float series = u + u * s * fmaf(s, fmaf(s, fmaf(s, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f);
+    return fabsf(u) < 0.25f ? out * series : capped_score(z, in, out);
 }
 
 // The page numbers and scales of 64 pages of a part, one to a lane: a page costs two register reads instead of two dependent trips to memory.
@@ -375,8 +393,7 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
     v4f o[D / 16];
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) o[d] = v4f{0.f, 0.f, 0.f, 0.f};
-    const bool capped = a.softcap > 0.f;
-    const float in_unit = (capped ? 2.f * LOG2E * a.scale / a.softcap : a.scale * LOG2E) * q_unit, cap_out = a.softcap * LOG2E;
+    const score_cap cap = cap_of(a, q_unit);
 
     int p = w.lo + wave;
     const EPARA_GLOBAL char* base = nullptr;
@@ -409,12 +426,19 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
         }
         if (more) load_keys(next);
         const int at = p * PAGE + 16 * q;                  // my keys are at + 4 t + i
-        float unit = in_unit * (q < 2 ? ps.key[0] : ps.key[1]);             // of a score, to log 2: my keys are of block q / 2
-        if (capped) {
+        float unit = cap.in * (q < 2 ? ps.key[0] : ps.key[1]);             // of a score, to log 2: my keys are of block q / 2
+        if (cap.on) {
+            if (cap.wide) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+                for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) z[t][i] = capped_score(z[t][i], unit, cap_out);
+                    for (int i = 0; i < 4; ++i) z[t][i] = widely_capped_score(z[t][i], unit, cap.out);
+            } else {
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z[t][i] = capped_score(z[t][i], unit, cap.out);
+            }
             unit = 1.f;
         }
         if (p * PAGE + PAGE - 1 > low_token || (a.window > 0 && p * PAGE <= high_token - a.window)) {
@@ -623,8 +647,7 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-    const bool capped = a.softcap > 0.f;
-    const float in_unit = (capped ? 2.f * LOG2E * a.scale / a.softcap : a.scale * LOG2E) * q_unit, cap_out = a.softcap * LOG2E;
+    const score_cap cap = cap_of(a, q_unit);
     // my rows see the pages [my_lo, my_hi) of the tile's; the others I only bring
     const int my_hi = live ? max_of(min_of(w.hi, (high_token + PAGE) / PAGE), w.lo) : w.lo;
     const int my_lo = min_of(my_hi, max_of(w.lo, a.window > 0 && low_token >= a.window ? (low_token - a.window + 1) / PAGE : 0));
@@ -677,14 +700,20 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
                 for (int u = 0; u < 2; ++u) z[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds8h(here + ((u * QS + s) * 2 + j) * 1024), query[s][j], z[u], 0, 0, 0);
         put(there);
         const uint32_t later = fetch(page_or_last(p + 2));
-        float unit[2] = {in_unit * ps.key[0], in_unit * ps.key[1]};          // of a score, to log 2
-        if (capped) {
+        float unit[2] = {cap.in * ps.key[0], cap.in * ps.key[1]};          // of a score, to log 2
+        if (cap.on) {
+            if (cap.wide) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
+                for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) z[u][i] = capped_score(z[u][i], unit[u], cap_out);
-                unit[u] = 1.f;
+                    for (int i = 0; i < 16; ++i) z[u][i] = widely_capped_score(z[u][i], unit[u], cap.out);
+            } else {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[u][i] = capped_score(z[u][i], unit[u], cap.out);
             }
+            unit[0] = unit[1] = 1.f;
         }
         if (p * PAGE + PAGE - 1 > low_token || (a.window > 0 && p * PAGE <= high_token - a.window)) {
             const int last = last_key - p * PAGE - 16 * h, from = first_key - p * PAGE - 16 * h;

@@ -84,3 +84,18 @@ def test_attention_of_values_at_the_end_of_the_range(rows):
         c = one_sequence(rng, n, rows, D, K, V, rng.standard_normal((rows, 2 * D)))
         run_attn([c])
         check_attn([c])
+
+
+@pytest.mark.parametrize("rows", [1, 90])
+@pytest.mark.parametrize("softcap", [1e-38, 1e-6, 500.0, 600.0, 1e3, 1e4, 1e5, 1e6, 1e8, 1e15, 1e25, 3e38])
+def test_attention_with_caps_far_from_the_scores(rows, softcap):
+    """A cap far above the scores leaves them what they are; under one far below them all keys weigh alike (but for their signs); scores of some hundreds about a cap of that size."""
+    for D in (64, 128):
+        n, rng = 200, np.random.default_rng([106, rows, D])
+        K, V = rng.standard_normal((n, 1, D)), rng.standard_normal((n, 1, D))
+        q = rng.standard_normal((rows, 2 * D))
+        q[0, :D] = 0.0
+        q[:, D:] *= 100.0 if softcap < 1e3 else 3.0
+        c = one_sequence(rng, n, rows, D, K, V, q, softcap=softcap)
+        run_attn([c])
+        check_attn([c])
