@@ -105,9 +105,9 @@ __global__ __launch_bounds__(NT) void add_rmsnorm_kernel(const epara_rmsnorm_arg
             }
         const epara_rmsnorm_args now = a;
         const size_t base = static_cast<size_t>(row - now.first_row) * now.d;
-        const int row_of_group = row - now.first_row, next = row + stride;
-        const bool more = next < n_rows && next > row;     // (a sum past 2^31 is negative)
-        if (more) load(next, a, group);
+        const int row_of_group = row - now.first_row;
+        const bool more = row < n_rows - stride;           // (row + stride may pass 2^31)
+        if (more) load(row + stride, a, group);
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int chunk = c * THREADS + at;
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(NT) void add_rmsnorm_kernel(const epara_rmsnorm_arg
             }
         }
         if (!more) return;
-        row = next;
+        row += stride;
     }
 }
 

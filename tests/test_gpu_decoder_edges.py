@@ -6,7 +6,7 @@ import torch
 
 from oracle import decoder as OD
 from paper_2511_00603_amd import runtime as R
-from test_gpu_decoder import BF, DEV, Case, check_attn, dev_bf16, fetch, run_attn, sync
+from test_gpu_decoder import DEV, SLACK, Case, check_attn, dev_bf16, run_attn, sync
 
 pytestmark = pytest.mark.gpu
 
@@ -99,3 +99,30 @@ def test_attention_with_caps_far_from_the_scores(rows, softcap):
         c = one_sequence(rng, n, rows, D, K, V, q, softcap=softcap)
         run_attn([c])
         check_attn([c])
+
+
+# ---- normalisation -----------------------------------------------------------------------------------------------
+
+def test_rmsnorm_of_as_many_rows_as_a_call_takes():
+    """2^31 - 1 rows in two groups: the last workgroups' next rows would pass 31 bits."""
+    counts, d, rng = [2**31 - 40001, 40000], 8, np.random.default_rng(111)
+    gamma = (1 + 0.2 * rng.standard_normal(d)).astype(np.float32)
+    groups, kept = [], []
+    for M in counts:
+        g = {"X": torch.zeros(M, d, dtype=torch.bfloat16, device=DEV), "gamma": torch.from_numpy(gamma).to(DEV), "eps": 1e-5, "out_scale": 0.01,
+             "Y": torch.full((M, d), 0x7F, dtype=torch.uint8, device=DEV)}
+        x, X = dev_bf16(rng.standard_normal((30000, d)))
+        for rows in (slice(0, 10000), slice(M // 2, M // 2 + 10000), slice(M - 10000, M)):
+            part = slice(10000 * (len(kept) % 3), 10000 * (len(kept) % 3) + 10000)
+            g["X"][rows] = X[part]
+            kept.append((g, rows, x[part]))
+        groups.append(g)
+    R.add_rmsnorm(R.RmsNormPlan(groups, DEV))
+    sync()
+    scale = float(np.float32(0.01))
+    for g, rows, x in kept:
+        _, y = OD.add_rms_norm(x, None, gamma.astype(np.float64), float(np.float32(1e-5)))
+        got, limit = OD.e4m3_decode(g["Y"][rows].cpu().numpy()) * scale, np.clip(y, -448 * scale, 448 * scale)
+        assert (np.abs(got - limit) <= np.maximum(np.abs(limit) * 2.0 ** -4, scale * 2.0 ** -10) * SLACK).all()
+    for g in groups:                                             # all other rows are zeros, and were written
+        assert not any((g["Y"][i: i + (1 << 28)] == 0x7F).any() for i in range(0, len(g["Y"]), 1 << 28))
