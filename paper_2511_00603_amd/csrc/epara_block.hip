@@ -185,19 +185,19 @@ __global__ __launch_bounds__(NT) void add_layernorm_kernel(const epara_norm_args
         norm_row_regs<CH> cur, nxt;
         norm_load<CH>(args, G, row, lane, first, cur);
         for (;;) {
-            const int next = row + stride;
-            const bool more = next < n_rows;
-            if (more) norm_load<CH>(args, G, next, lane, first, nxt);
+            const bool more = row < n_rows - stride;      // (row + stride may pass 2^31)
+            if (more) norm_load<CH>(args, G, row + stride, lane, first, nxt);
             norm_finish<CH>(cur, lane);
             if (!more) break;
             cur = nxt;
-            row = next;
+            row += stride;
         }
     } else {                                              // a wide row alone is 8 KiB or more of loads in flight
-        for (; row < n_rows; row += stride) {
+        for (;; row += stride) {
             norm_row_regs<CH> cur;
             norm_load<CH>(args, G, row, lane, first, cur);
             norm_finish<CH>(cur, lane);
+            if (row >= n_rows - stride) break;
         }
     }
 }
