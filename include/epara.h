@@ -847,10 +847,11 @@ int32_t epara_attention(const epara_attn_args* h_args, const epara_attn_args* d_
 /* Rows of one service through a residual connection and a root-mean-square normalisation (Zhang and Sennrich 2019):
  * s = x + r per element (r absent: s = x), then per row of d values y = s / sqrt(mean(s^2) + eps) * gamma.  The
  * statistic and y come from the unrounded fp32 sum; S receives the sum rounded to bf16.  Y is bf16, or E4M3 codes:
- *   row_scales given: a row's scale is max |y| / 448 (1 for a row of zeros), code = sat(RNE(y * (1 / scale)));
+ *   row_scales given: a row's scale is max |y| / 448 (1 for a row of zeros, and 2^-126 at least), code = sat(RNE(y * (1 / scale)));
  *   row_scales NULL:  code = sat(RNE(y * out_inv_scale)), the service's static scale: what a grouped forward with
  *                     scale = s_x * s_w reads.
- * A row that holds a NaN or an infinity gets unspecified codes and a scale that is not finite.  72 bytes. */
+ * Rows of any finite size are normalised; with eps = 0 a row of zeros stays zeros.  A row that holds a NaN or an infinity (a sum that passes
+ * fp32's range is one) gets unspecified codes and a scale that is not finite.  72 bytes. */
 typedef struct {
     const void*  X;              /* device, bf16 [M, d] row-major, 16-byte aligned */
     const void*  R;              /* device, bf16 [M, d], or NULL */

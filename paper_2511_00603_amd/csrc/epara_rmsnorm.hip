@@ -3,7 +3,8 @@
 //   s = x + r,  y = s / sqrt(mean(s^2) + eps) * gamma;   8 bits: code = sat(RNE(y / scale))
 //
 // A wave or a workgroup per row: the row is read once and stays in registers; its sum of squares and (8 bits with a scale per row) the
-// maximum of |s gamma| are reduced together, since max |y| = max |s gamma| / sqrt(..).
+// maximum of |s gamma| are reduced together, since max |y| = max |s gamma| / sqrt(..).  A row whose squares leave fp32's range (values from 2^57 on, or
+// all under 2^-48 with an eps no larger than their squares) is taken once more, from the registers, with its power of two taken out.
 // Bound by HBM: 8192 rows of 5120 in bf16 64 us (5.2 TB/s), in 8 bits with a scale per row 57 us (5.1 TB/s); with a wave per row, whose 80 chunks
 // leave room for one wave per SIMD, 96 and 91.  105 rows of 4096 (a launch and its trips to memory) 3.5 us alone, 6.1 with a wave per row.
 #include <hip/hip_runtime.h>
@@ -44,6 +45,9 @@ __device__ __forceinline__ int find_group(const epara_rmsnorm_args* __restrict__
     return lo;
 }
 
+constexpr float LEAST_MEAN = 0x1p-96f;                     // of s^2, plus eps: above, what underflows in the squares does not count
+constexpr float LEAST_SCALE = 0x1p-126f;                   // of a row's codes: the smallest whose inverse is finite
+
 // THREADS threads share a row (64: a wave, narrow rows; 256: a workgroup), CH = 16-byte chunks (8 values) of it per thread that the widest row of
 // the launch needs.  The loads of the next row are in flight while one is reduced and stored, and gamma stays in registers for as long as the
 // rows are of one service.
@@ -52,6 +56,7 @@ __global__ __launch_bounds__(NT) void add_rmsnorm_kernel(const epara_rmsnorm_arg
 {
     constexpr int ROWS = NT / THREADS, WAVES = THREADS / 64;
     __shared__ float part[2][2][WAVES];                    // [turn][sum, maximum][wave]
+    __shared__ float again[3][WAVES];                      // of a row that is taken once more: [largest value, sum, maximum][wave]
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int at = THREADS == 64 ? lane : static_cast<int>(threadIdx.x);           // my place in the row
@@ -118,11 +123,9 @@ __global__ __launch_bounds__(NT) void add_rmsnorm_kernel(const epara_rmsnorm_arg
                 for (int j = 0; j < 4; ++j) out[j] = static_cast<int>(pack_bf16(s[c][2 * j], s[c][2 * j + 1]));
                 *reinterpret_cast<EPARA_GLOBAL v4i*>((EPARA_GLOBAL char*)now.S + base * 2 + chunk * 16) = out;
             }
+            if constexpr (BITS8)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                s[c][j] *= gm[c][j >> 2][j & 3];
-                if constexpr (BITS8) top = fmaxf(top, fabsf(s[c][j]));
-            }
+                for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(s[c][j] * gm[c][j >> 2][j & 3]));
         }
 #pragma unroll
         for (int d = 32; d >= 1; d >>= 1) {
@@ -144,11 +147,45 @@ __global__ __launch_bounds__(NT) void add_rmsnorm_kernel(const epara_rmsnorm_arg
             }
             turn ^= 1;
         }
-        float factor = 1.f / sqrtf(sum / static_cast<float>(now.d) + now.eps);
+        float mean = sum / static_cast<float>(now.d) + now.eps;
+        if (!(mean < INFINITY) || mean < LEAST_MEAN) {     // (the same for all threads of the row)
+            auto all = [&](float x, int which, bool add) {
+#pragma unroll
+                for (int d = 32; d >= 1; d >>= 1) x = add ? x + __shfl_xor(x, d) : fmaxf(x, __shfl_xor(x, d));
+                if constexpr (WAVES > 1) {
+                    if (lane == 0) again[which][wave] = x;
+                    __syncthreads();
+                    x = again[which][0];
+#pragma unroll
+                    for (int i = 1; i < WAVES; ++i) x = add ? x + again[which][i] : fmaxf(x, again[which][i]);
+                }
+                return x;
+            };
+            float largest = 0.f;
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) largest = fmaxf(largest, fabsf(s[c][j]));
+            largest = fmaxf(all(largest, 0, false), sqrtf(now.eps));
+            const int e = static_cast<int>(__float_as_uint(largest) >> 23) - 127;       // 0: -127
+            sum = top = 0.f;
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    s[c][j] = __builtin_ldexpf(s[c][j], -e);
+                    sum += s[c][j] * s[c][j];
+                    if (BITS8 && c * THREADS + at < n_chunks) top = fmaxf(top, fabsf(s[c][j] * gm[c][j >> 2][j & 3]));
+                }
+            mean = all(sum, 1, true) / static_cast<float>(now.d) + __builtin_ldexpf(now.eps, -2 * e);
+            if constexpr (BITS8) top = all(top, 2, false);
+        }
+        const float factor = mean == 0.f ? 0.f : 1.f / sqrtf(mean);         // a row of zeros stays one
         if constexpr (BITS8) {
             float inv = now.out_inv_scale;
             if (now.row_scales) {
-                const float scale = top * factor == 0.f ? 1.f : top * factor / 448.f;    // a NaN in the row is a NaN here
+                float scale = top * factor == 0.f ? 1.f : top * factor / 448.f;          // a NaN in the row is a NaN here
+                if (scale < LEAST_SCALE) scale = LEAST_SCALE;
                 inv = 1.f / scale;
                 if (at == 0) ((EPARA_GLOBAL float*)now.row_scales)[row_of_group] = scale;
             }
@@ -158,7 +195,7 @@ __global__ __launch_bounds__(NT) void add_rmsnorm_kernel(const epara_rmsnorm_arg
                 if (chunk >= n_chunks) continue;
                 float y[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] = s[c][j] * factor * inv;
+                for (int j = 0; j < 8; ++j) y[j] = s[c][j] * gm[c][j >> 2][j & 3] * factor * inv;
                 const v2u codes = {epara_cast::f32x4_to_e4m3(y[0], y[1], y[2], y[3]), epara_cast::f32x4_to_e4m3(y[4], y[5], y[6], y[7])};
                 *reinterpret_cast<EPARA_GLOBAL v2u*>((EPARA_GLOBAL char*)now.Y + base + chunk * 8) = codes;
             }
@@ -169,7 +206,10 @@ __global__ __launch_bounds__(NT) void add_rmsnorm_kernel(const epara_rmsnorm_arg
                 if (chunk >= n_chunks) continue;
                 v4i out;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) out[j] = static_cast<int>(pack_bf16(s[c][2 * j] * factor, s[c][2 * j + 1] * factor));
+                for (int j = 0; j < 4; ++j) {
+                    const int e = 2 * j, o = e + 1;
+                    out[j] = static_cast<int>(pack_bf16(s[c][e] * gm[c][e >> 2][e & 3] * factor, s[c][o] * gm[c][o >> 2][o & 3] * factor));
+                }
                 *reinterpret_cast<EPARA_GLOBAL v4i*>((EPARA_GLOBAL char*)now.Y + base * 2 + chunk * 16) = out;
             }
         }

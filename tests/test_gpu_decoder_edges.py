@@ -6,7 +6,7 @@ import torch
 
 from oracle import decoder as OD
 from paper_2511_00603_amd import runtime as R
-from test_gpu_decoder import DEV, SLACK, Case, check_attn, dev_bf16, run_attn, sync
+from test_gpu_decoder import BF, DEV, SLACK, Case, check_attn, dev_bf16, fetch, run_attn, sync
 
 pytestmark = pytest.mark.gpu
 
@@ -126,3 +126,43 @@ def test_rmsnorm_of_as_many_rows_as_a_call_takes():
         assert (np.abs(got - limit) <= np.maximum(np.abs(limit) * 2.0 ** -4, scale * 2.0 ** -10) * SLACK).all()
     for g in groups:                                             # all other rows are zeros, and were written
         assert not any((g["Y"][i: i + (1 << 28)] == 0x7F).any() for i in range(0, len(g["Y"]), 1 << 28))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "row", "service"])
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-5])
+@pytest.mark.parametrize("with_r", [True, False])
+def test_rmsnorm_of_rows_of_any_size(kind, eps, with_r):
+    """Rows of zeros, rows whose squares pass fp32's range at either end, and ordinary ones side by side; a row of one large value."""
+    rng, groups, want = np.random.default_rng([113, with_r]), [], []
+    sizes = np.array([0.0, 1e-38, 1e-30, 1e-25, 1e-19, 1.0, 1e18, 3e19, 1e30, 5e37, 0.0, 1.0])
+    for d in (8, 520, 1032, 8192):
+        x, X = dev_bf16(rng.standard_normal((len(sizes), d)) * sizes[:, None])
+        r, Rt = dev_bf16(rng.standard_normal((len(sizes), d)) * 0.5 * sizes[:, None]) if with_r else (None, None)
+        X[-1, 5] = 2.0 ** 100
+        x[-1, 5] = 2.0 ** 100
+        gamma = (1 + 0.2 * rng.standard_normal(d)).astype(np.float32)
+        g = {"X": X, "R": Rt, "gamma": torch.from_numpy(gamma).to(DEV), "S": torch.full_like(X, 7.0), "eps": eps,
+             "Y": torch.full((len(sizes), d), 7.0, dtype=torch.bfloat16, device=DEV) if kind == "bf16" else torch.full((len(sizes), d), 0x7F, dtype=torch.uint8, device=DEV)}
+        if kind == "row":
+            g["row_scales"] = torch.full((len(sizes),), -1.0, device=DEV)
+        if kind == "service":
+            g["out_scale"] = 0.011
+        s = x if r is None else x + r
+        e = float(np.float32(eps))
+        root = np.sqrt((s * s).mean(axis=1, keepdims=True) + e)
+        groups.append(g)
+        want.append((s, np.divide(s, root, out=np.zeros_like(s), where=root > 0) * gamma))
+    R.add_rmsnorm(R.RmsNormPlan(groups, DEV))
+    sync()
+    for g, (s, y) in zip(groups, want):
+        assert (np.abs(fetch(g["S"]) - s) <= BF * np.abs(s) + 1e-40).all()
+        if kind == "bf16":
+            assert (np.abs(fetch(g["Y"]) - y) <= BF * np.abs(y) + 1e-40).all()
+            continue
+        scale = np.full((len(y), 1), float(np.float32(0.011)))
+        if kind == "row":
+            scale, top = fetch(g["row_scales"])[:, None], np.abs(y).max(axis=1, keepdims=True)
+            least = np.where(top > 0, np.maximum(top / 448.0, 2.0 ** -126), 1.0)
+            assert (np.abs(scale - least) <= 1e-6 * least).all()
+        got, limit = OD.e4m3_decode(g["Y"].cpu().numpy()) * scale, np.clip(y, -448 * scale, 448 * scale)
+        assert (np.abs(got - limit) <= np.maximum(np.abs(limit) * 2.0 ** -4, scale * 2.0 ** -10) * SLACK).all()
