@@ -937,7 +937,7 @@ typedef struct {
  * Rotation, maxima and products are fp32.  h_first / d_first: int32[n_seqs + 1] from epara_plan_cache_append (running sums
  * of the work of the sequences).  No rows: nothing is enqueued.
  * Errors: ERR_NULL; ERR_SHAPE (a dimension out of range, a stride shorter than a row, rows outside the service's, positions outside
- * the page table or (without `positions`) the rotary table, a page outside the cache, a page that two sequences of the call write,
+ * the page table or (without `positions`) the rotary table, a page outside the cache, a page or a row of Q that two sequences of the call write,
  * sequences not ordered by service, h_first not the plan's); ERR_ALIGN; ERR_CAPACITY (too much work for one grid, or no host memory). */
 int32_t epara_plan_cache_append(const epara_append_args* h_args, int32_t G, const epara_sequence_table* table, int32_t* first);
 int32_t epara_cache_append(const epara_append_args* h_args, const epara_append_args* d_args, int32_t G, const epara_sequence_table* table,
@@ -989,8 +989,8 @@ typedef struct {
  * the largest weight times its block's scale.  They keep their bits down to 2^-23 of that, and 2^-33 is the last that counts; keys that a row does
  * not see take no part.  One kernel for sequences with few rows to a key head, one for those with many; a long context is cut into parts that
  * run side by side, and the last of them to end adds them up in order: results do not depend on timing.
- * Errors as for epara_cache_append; also ERR_SHAPE for a scale or softcap that is negative or not finite, O the same buffer as Q, or a
- * plan that is not this call's, ERR_CAPACITY for a workspace that is too small. */
+ * Errors as for epara_cache_append; also ERR_SHAPE for a scale or softcap that is negative or not finite, O the same buffer as Q, a
+ * row of two sequences, or a plan that is not this call's, ERR_CAPACITY for a workspace that is too small. */
 int32_t epara_plan_cache_attention(const epara_cache_attn_args* h_args, int32_t G, const epara_sequence_table* table, int32_t n_compute_units,
                                    int32_t* first, epara_cache_attn_plan* plan);
 int32_t epara_cache_attention(const epara_cache_attn_launch* launch, void* stream);

@@ -79,6 +79,32 @@ int32_t check_append(const epara_append_args* args, int32_t G, const epara_seque
     return EPARA_OK;
 }
 
+// No row is written for two sequences of a service; writes(args): whether that service's rows are.  Sequences in the order of their rows, as a rule, need no list.
+template <class Args, class Writes>
+int32_t check_rows_once(const Args* args, const epara_sequence_table* t, Writes writes)
+{
+    bool ordered = true;
+    int32_t service = -1, end = 0;
+    for (int32_t i = 0; i < t->n_seqs && ordered; ++i) {
+        const epara_sequence& s = t->h_seqs[i];
+        if (s.rows == 0 || !writes(args[s.service])) continue;
+        ordered = s.service != service || s.first_row >= end;
+        service = s.service;
+        end = s.first_row + s.rows;
+    }
+    if (ordered) return EPARA_OK;
+    try {
+        std::vector<epara_sequence> seqs;
+        for (int32_t i = 0; i < t->n_seqs; ++i)
+            if (t->h_seqs[i].rows > 0 && writes(args[t->h_seqs[i].service])) seqs.push_back(t->h_seqs[i]);
+        std::sort(seqs.begin(), seqs.end(), [](const epara_sequence& a, const epara_sequence& b) { return a.service != b.service ? a.service < b.service : a.first_row < b.first_row; });
+        const auto meet = [](const epara_sequence& a, const epara_sequence& b) { return a.service == b.service && b.first_row < a.first_row + a.rows; };
+        return std::adjacent_find(seqs.begin(), seqs.end(), meet) == seqs.end() ? EPARA_OK : EPARA_ERR_SHAPE;
+    } catch (const std::bad_alloc&) {
+        return EPARA_ERR_CAPACITY;
+    }
+}
+
 // No page of a cache is written for two sequences (or twice for one).
 int32_t check_written_once(const epara_append_args* args, const epara_sequence_table* t)
 {
@@ -194,6 +220,7 @@ int32_t epara_check_append_call(const epara_append_args* h_args, int32_t G, cons
     if (table->n_seqs > 0 && !h_first) return EPARA_ERR_NULL;
     if (table->n_seqs == 0) return EPARA_OK;
     if (const int32_t rc = count_append(h_args, table, nullptr, h_first)) return rc;
+    if (const int32_t rc = check_rows_once(h_args, table, [](const epara_append_args& a) { return a.Q != nullptr; })) return rc;
     return check_written_once(h_args, table);
 }
 
@@ -207,6 +234,7 @@ int32_t epara_check_attn_call(const epara_cache_attn_launch& l, bool cut[2])
     int32_t n[2];
     if (const int32_t rc = count_attn(l.h_args, &l.table, l.plan.part_pages, nullptr, l.h_first, n, cut)) return rc;
     if (n[0] != l.plan.n_items[0] || n[1] != l.plan.n_items[1]) return EPARA_ERR_SHAPE;
+    if (const int32_t rc = check_rows_once(l.h_args, &l.table, [](const epara_cache_attn_args&) { return true; })) return rc;
     const int64_t bytes = attn_workspace(n, cut);
     if (bytes > 0) {
         if (!l.d_workspace) return EPARA_ERR_NULL;

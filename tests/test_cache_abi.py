@@ -320,3 +320,40 @@ def test_cache_host_code_is_clean_under_asan_and_ubsan(tmp_path):
     env.pop("LD_PRELOAD", None)
     r = subprocess.run([exe], env=env, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
     assert r.returncode == 0 and "sanitize_cache: ok" in r.stdout and "runtime error" not in r.stdout, r.stdout[-4000:]
+
+
+def test_rows_that_two_sequences_would_write_are_refused():
+    """Two sequences of a service with a row in common would write it in a race: attention's output, and an append's queries.  Rows that are only read may be shared, in any order."""
+    L = B.lib()
+
+    def attention(seqs, pages=range(8)):
+        args = attn_args(rows=20)
+        rc, first, plan = attn_plan(args, seqs, pages)
+        assert rc == B.EPARA_OK
+        t, keep = table_of(seqs, list(pages))
+        # no device arguments: a call that is not refused ends there, before it enqueues anything
+        launch = B.CacheAttnLaunch(args.ctypes.data, None, first.ctypes.data, D, None, 0, t, plan, 1, 0)
+        return L.epara_cache_attention(ctypes.addressof(launch), None)
+
+    def append(seqs, **kw):
+        args = append_args(rows=20, **kw)
+        t, keep = table_of(seqs, list(range(8)))
+        first = np.zeros(len(seqs) + 1, dtype=np.int32)
+        assert L.epara_plan_cache_append(args.ctypes.data, 1, ctypes.addressof(t), first.ctypes.data) == B.EPARA_OK
+        return L.epara_cache_append(args.ctypes.data, None, 1, ctypes.addressof(t), first.ctypes.data, D, None)
+
+    seq = lambda row, rows, page: (0, row, rows, 10, page, 1)
+    apart = [[seq(0, 3, 0), seq(3, 4, 1), seq(7, 1, 2)], [seq(7, 1, 2), seq(0, 3, 0), seq(3, 4, 1)], [seq(5, 0, 0), seq(3, 4, 1), seq(5, 0, 2), seq(19, 1, 3)]]
+    shared = [[seq(0, 3, 0), seq(2, 4, 1)], [seq(2, 4, 0), seq(0, 3, 1)], [seq(5, 2, 0), seq(0, 20, 1)], [seq(8, 1, 0), seq(2, 1, 1), seq(8, 1, 2)]]
+    for s in apart:
+        assert attention(s) == B.EPARA_ERR_NULL and append(s) == B.EPARA_ERR_NULL, s
+    for s in shared:
+        assert attention(s) == B.EPARA_ERR_SHAPE and append(s) == B.EPARA_ERR_SHAPE, s
+        assert append(s, Q=0, rotary=0) == B.EPARA_ERR_NULL, s
+    # rows of two services are rows of two tensors
+    args = np.concatenate([attn_args(), attn_args()])
+    t, keep = table_of([(0, 0, 3, 10, 0, 1), (1, 0, 3, 10, 1, 1)], [1, 2])
+    first, p = np.zeros(6, dtype=np.int32), B.CacheAttnPlan()
+    assert L.epara_plan_cache_attention(args.ctypes.data, 2, ctypes.addressof(t), 256, first.ctypes.data, ctypes.addressof(p)) == B.EPARA_OK
+    launch = B.CacheAttnLaunch(args.ctypes.data, None, first.ctypes.data, D, None, 0, t, p, 2, 0)
+    assert L.epara_cache_attention(ctypes.addressof(launch), None) == B.EPARA_ERR_NULL
