@@ -1007,7 +1007,7 @@ typedef struct {
 } epara_page_copy;
 
 /* One kernel on `stream`.  Errors: ERR_NULL; ERR_SHAPE (a dimension out of range, a page outside the cache, a destination that is
- * used twice or is also a source, moves outside the list, first_chunk not the running sum); ERR_ALIGN; ERR_CAPACITY (no host memory). */
+ * used twice or is also a source (in all entries of one cache together), moves outside the list, first_chunk not the running sum); ERR_ALIGN; ERR_CAPACITY (no host memory). */
 int32_t epara_copy_pages(const epara_page_copy* h_caches, const epara_page_copy* d_caches, int32_t G,
                          const epara_page_move* h_moves, const epara_page_move* d_moves, int32_t n_moves, void* stream);
 

@@ -7,6 +7,7 @@
 #include <algorithm>
 #include <climits>
 #include <cmath>
+#include <functional>
 #include <new>
 #include <vector>
 
@@ -244,6 +245,29 @@ int32_t epara_check_attn_call(const epara_cache_attn_launch& l, bool cut[2])
     return EPARA_OK;
 }
 
+namespace {
+
+// The moves of caches[order[0 .. n)], which are one cache: no page is twice a destination, or a destination and a source.  used: scratch.
+int32_t check_moves(const epara_page_copy* caches, const int32_t* order, int32_t n, const epara_page_move* moves, std::vector<char>& used)
+{
+    const epara_page_copy& one = caches[order[0]];
+    used.assign(static_cast<size_t>(one.n_pages), 0);            // per page: 1 a source, 2 a destination
+    for (int32_t k = 0; k < n; ++k) {
+        const epara_page_copy& c = caches[order[k]];
+        if (c.n_pages != one.n_pages || c.kv_heads != one.kv_heads || c.head_dim != one.head_dim) return EPARA_ERR_SHAPE;
+        for (int32_t i = c.first_move; i < c.first_move + c.n_moves; ++i) {
+            const epara_page_move& m = moves[i];
+            if (m.src < 0 || m.src >= c.n_pages || m.dst < 0 || m.dst >= c.n_pages || m.src == m.dst) return EPARA_ERR_SHAPE;
+            if (used[static_cast<size_t>(m.src)] == 2 || used[static_cast<size_t>(m.dst)] != 0) return EPARA_ERR_SHAPE;
+            used[static_cast<size_t>(m.src)] = 1;
+            used[static_cast<size_t>(m.dst)] = 2;
+        }
+    }
+    return EPARA_OK;
+}
+
+}  // namespace
+
 int32_t epara_check_copy_call(const epara_page_copy* caches, int32_t G, const epara_page_move* moves, int32_t n_moves, int32_t* n_chunks)
 {
     *n_chunks = 0;
@@ -252,7 +276,8 @@ int32_t epara_check_copy_call(const epara_page_copy* caches, int32_t G, const ep
     if (!caches || (n_moves > 0 && !moves)) return EPARA_ERR_NULL;
     int64_t chunks = 0;
     try {
-        std::vector<char> used;                                  // per page: 1 a source, 2 a destination
+        std::vector<char> used;
+        std::vector<int32_t> order;                              // caches with moves
         for (int32_t g = 0; g < G; ++g) {
             const epara_page_copy& c = caches[g];
             if (bad_heads(c.kv_heads, c.kv_heads, c.head_dim, c.n_pages) || c.first_move < 0 || c.n_moves < 0 || static_cast<int64_t>(c.first_move) + c.n_moves > n_moves) return EPARA_ERR_SHAPE;
@@ -262,16 +287,17 @@ int32_t epara_check_copy_call(const epara_page_copy* caches, int32_t G, const ep
             if (c.n_moves == 0) continue;
             if (!c.codes || !c.scales) return EPARA_ERR_NULL;
             if (misaligned(c.codes, 16) || misaligned(c.scales, 4)) return EPARA_ERR_ALIGN;
+            order.push_back(g);
             // the layers of a service follow each other with the same moves and as many pages: looked at once
             if (g > 0 && caches[g - 1].first_move == c.first_move && caches[g - 1].n_moves == c.n_moves && caches[g - 1].n_pages == c.n_pages) continue;
-            used.assign(static_cast<size_t>(c.n_pages), 0);
-            for (int32_t i = c.first_move; i < c.first_move + c.n_moves; ++i) {
-                const epara_page_move& m = moves[i];
-                if (m.src < 0 || m.src >= c.n_pages || m.dst < 0 || m.dst >= c.n_pages || m.src == m.dst) return EPARA_ERR_SHAPE;
-                if (used[static_cast<size_t>(m.src)] == 2 || used[static_cast<size_t>(m.dst)] != 0) return EPARA_ERR_SHAPE;
-                used[static_cast<size_t>(m.src)] = 1;
-                used[static_cast<size_t>(m.dst)] = 2;
-            }
+            if (const int32_t rc = check_moves(caches, &g, 1, moves, used)) return rc;
+        }
+        // entries of the same cache are looked at together
+        std::sort(order.begin(), order.end(), [caches](int32_t a, int32_t b) { return std::less<const void*>()(caches[a].codes, caches[b].codes); });
+        for (size_t at = 0, end; at < order.size(); at = end) {
+            for (end = at + 1; end < order.size() && caches[order[end]].codes == caches[order[at]].codes;) ++end;
+            if (end == at + 1) continue;
+            if (const int32_t rc = check_moves(caches, &order[at], static_cast<int32_t>(end - at), moves, used)) return rc;
         }
     } catch (const std::bad_alloc&) {
         return EPARA_ERR_CAPACITY;

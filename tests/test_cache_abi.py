@@ -357,3 +357,29 @@ def test_rows_that_two_sequences_would_write_are_refused():
     assert L.epara_plan_cache_attention(args.ctypes.data, 2, ctypes.addressof(t), 256, first.ctypes.data, ctypes.addressof(p)) == B.EPARA_OK
     launch = B.CacheAttnLaunch(args.ctypes.data, None, first.ctypes.data, D, None, 0, t, p, 2, 0)
     assert L.epara_cache_attention(ctypes.addressof(launch), None) == B.EPARA_ERR_NULL
+
+
+def test_copies_that_collide_in_a_cache_named_twice_are_refused():
+    """A cache may come in several entries; their moves are then those of one cache: a destination twice, or a source of another entry, is a race."""
+    L = B.lib()
+
+    def call(*entries):
+        """entries: (codes, moves); without device arguments a call that is not refused ends there."""
+        moves, c, chunks = [m for _, own in entries for m in own], np.zeros(len(entries), dtype=B.PAGE_COPY), 0
+        for i, (codes, own) in enumerate(entries):
+            c[i] = (codes, codes + 0x10000, 10, 2, 128, sum(len(o) for _, o in entries[:i]), len(own), chunks)
+            chunks += 2 * len(own)
+        m = np.array(moves, dtype=B.PAGE_MOVE)
+        return L.epara_copy_pages(c.ctypes.data, None, len(c), m.ctypes.data, None, len(m), None)
+
+    other = D + 0x100000
+    for entries in ([(D, [(1, 2)]), (D, [(3, 4)])], [(D, [(1, 2)]), (other, [(1, 2)]), (D, [(1, 5)])], [(D, []), (D, [(1, 2)]), (D, [])]):
+        assert call(*entries) == B.EPARA_ERR_NULL, entries
+    for second in ([(3, 2)], [(2, 3)], [(5, 1)], [(1, 2)], [(6, 7), (4, 2)]):
+        assert call((D, [(1, 2)]), (D, second)) == B.EPARA_ERR_SHAPE, second
+        assert call((D, second), (other, [(0, 9)]), (D, [(1, 2)])) == B.EPARA_ERR_SHAPE, second
+    # the same list for a cache that is named twice, and entries that see the cache's pages differently
+    c, m = np.zeros(2, dtype=B.PAGE_COPY), np.array([(1, 2)], dtype=B.PAGE_MOVE)
+    for second in ((D, D, 10, 2, 128, 0, 1, 2), (D, D, 10, 4, 64, 0, 1, 2)):
+        c[0], c[1] = (D, D, 10, 2, 128, 0, 1, 0), second
+        assert L.epara_copy_pages(c.ctypes.data, None, 2, m.ctypes.data, None, 1, None) == B.EPARA_ERR_SHAPE
