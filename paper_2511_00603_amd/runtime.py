@@ -404,6 +404,8 @@ class CacheAppendPlan:
             qkv = _want(g["QKV"], bf, (rows, (H + 2 * c.kv_heads) * D), "QKV", strided=True)
             Q, rotary, positions = g.get("Q"), g.get("rotary"), g.get("positions")
             pairs = [int(v) for v in g.get("axis_pairs") or (D // 2, 0, 0)]
+            if rotary is not None and rotary.shape[0] == 0:
+                raise ValueError("rotary: a table without positions")
             if len(pairs) != 3 or min(pairs) < 0 or sum(pairs) != D // 2:
                 raise ValueError("axis_pairs: three counts that make %d" % (D // 2))
             self.args[i] = (qkv, _want(Q, bf, (rows, H * D), "Q", True, True), c.codes.data_ptr(), c.scales.data_ptr(),
@@ -436,7 +438,7 @@ class CacheAttnPlan:
             rows, D = int(g["Q"].shape[0]), c.head_dim
             self.args[i] = (_want(g["Q"], bf, (rows, H * D), "Q", strided=True), _want(g["O"], bf, (rows, H * D), "O", strided=True),
                             c.codes.data_ptr(), c.scales.data_ptr(), rows, H, c.kv_heads, D, c.n_pages, _row_stride(g["Q"]), _row_stride(g["O"]),
-                            int(g.get("window") or 0), float(g.get("scale") or D ** -0.5), float(g.get("softcap") or 0.0), (0, 0))
+                            int(g.get("window") or 0), D ** -0.5 if g.get("scale") is None else float(g["scale"]), float(g.get("softcap") or 0.0), (0, 0))
         self.first, self.plan = B.epara_plan_cache_attention(self.args, table.c, n_compute_units(device))
         self.d_args, self.d_first = _upload_all([self.args, self.first], device)
         self.d_workspace, at = None, 0

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from paper_2511_00603_amd import binding as B
+from paper_2511_00603_amd import runtime as R
 from test_gpu_decoder_block import DEV, Checked
 from workloads import make_mix
 
@@ -28,3 +29,21 @@ def test_decoder_block_after_refused_steps():
     blk.release(1, "b4")
     c.step([[("a", X(7))], [("b0", X(3)), ("e", X(300))], [("d", X(1))]])                         # the first of them again
     c.step([[("a", X(1))], [("e", X(1)), ("b0", X(1)), ("b3", X(1))], []])
+
+
+def test_plans_do_not_take_an_empty_table_or_a_scale_of_nothing_for_one_left_out():
+    cache = R.PagedCache.empty(2, 1, 64, DEV)
+    QKV, Q, O = (torch.zeros(3, n * 64, dtype=torch.bfloat16, device=DEV) for n in (4, 2, 2))
+    table = R.SequenceTable([[{"first_row": 0, "rows": 3, "start": 0, "pages": [0]}]], DEV)
+    append = {"QKV": QKV, "Q": Q, "cache": cache, "heads": 2}
+    for rows in (0, 2):                                          # fewer angles than positions
+        with pytest.raises((ValueError, B.EparaError)):
+            R.CacheAppendPlan(table, [dict(append, rotary=torch.zeros(rows, 32, 2, device=DEV))], DEV)
+    R.CacheAppendPlan(table, [dict(append, rotary=torch.zeros(3, 32, 2, device=DEV))], DEV)
+    attn = {"Q": Q, "O": O, "cache": cache, "heads": 2}
+    for scale in (0, 0.0, -1.0):
+        with pytest.raises(B.EparaError):
+            R.CacheAttnPlan(table, [dict(attn, scale=scale)], DEV)
+    for scale in (None, 0.25):
+        plan = R.CacheAttnPlan(table, [dict(attn, scale=scale)], DEV)
+        assert plan.args[0]["scale"] == np.float32(scale or 0.125)
