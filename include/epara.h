@@ -1029,7 +1029,7 @@ int32_t epara_pages_take(epara_page_pool* pool, int32_t n, int32_t* pages);
 /* A second sequence that begins like one of `tokens` tokens in `pages`: child[i] is its page i for all ceil(tokens / 64) of them.  Whole
  * pages are shared (one holder more); a part-filled last page, which both will write, is a fresh one and *n_moves = 1 with the
  * copy that epara_copy_pages has to make in moves[0]; otherwise *n_moves = 0.  ERR_CAPACITY (and nothing changed) if no page is free
- * for it; ERR_SHAPE for pages that nobody holds. */
+ * for it; ERR_SHAPE for pages that nobody holds.  Whole pages of -1, which a window has left behind, stay -1. */
 int32_t epara_pages_fork(epara_page_pool* pool, const int32_t* pages, int32_t tokens, int32_t* child, epara_page_move* move, int32_t* n_moves);
 
 /* One holder less for each of pages[0 .. n); a page without holders is free again.  Entries of -1 (pages that a window has

@@ -170,7 +170,8 @@ class Pages:
     def fork(self, pages, tokens):
         whole, n = tokens // PAGE, -(-tokens // PAGE)
         for p in pages[:whole]:
-            self.refs[p] += 1
+            if p != -1:
+                self.refs[p] += 1
         child, moves = list(pages[:whole]), []
         if n > whole:
             child += self.take(1)

@@ -373,12 +373,14 @@ int32_t epara_pages_fork(epara_page_pool* pool, const int32_t* pages, int32_t to
     const int32_t n = static_cast<int32_t>(ceil_div(tokens, PAGE)), whole = tokens / PAGE;
     if (n > 0 && (!pages || !child)) return EPARA_ERR_NULL;
     if (n > whole && !move) return EPARA_ERR_NULL;
-    for (int32_t i = 0; i < n; ++i)
+    for (int32_t i = 0; i < n; ++i) {
+        if (pages[i] == -1 && i < whole) continue;
         if (pages[i] < 0 || pages[i] >= pool->n_pages || pool->refs[pages[i]] < 1 || pool->refs[pages[i]] == INT32_MAX) return EPARA_ERR_SHAPE;
+    }
     if (n > whole && pool->n_free < 1) return EPARA_ERR_CAPACITY;
     for (int32_t i = 0; i < whole; ++i) {
         child[i] = pages[i];
-        ++pool->refs[pages[i]];
+        if (pages[i] != -1) ++pool->refs[pages[i]];
     }
     if (n > whole) {
         const int32_t src = pages[whole];

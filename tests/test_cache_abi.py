@@ -383,3 +383,30 @@ def test_copies_that_collide_in_a_cache_named_twice_are_refused():
     for second in ((D, D, 10, 2, 128, 0, 1, 2), (D, D, 10, 4, 64, 0, 1, 2)):
         c[0], c[1] = (D, D, 10, 2, 128, 0, 1, 0), second
         assert L.epara_copy_pages(c.ctypes.data, None, 2, m.ctypes.data, None, 1, None) == B.EPARA_ERR_SHAPE
+
+
+def test_sequences_whose_window_has_left_pages_behind_fork_too():
+    """Entries of -1 stand for pages that were given back, for fork as for free and compact; a part-filled last page has to be there."""
+    pool, refs, free = pool_of(8)
+    ref = OD.Pages(8)
+    pages = B.epara_pages_take(pool, 4).tolist()
+    assert pages == ref.take(4)
+    B.epara_pages_free(pool, pages[:2])
+    ref.free(pages[:2])
+    left = [-1, -1] + pages[2:]
+    for tokens in (256, 250, 192, 128, 100):
+        if tokens == 100:                                        # its last page, of which 36 tokens are the child's, is gone
+            before = refs.copy(), pool.n_free
+            with pytest.raises(B.EparaError) as e:
+                B.epara_pages_fork(pool, left, tokens)
+            assert e.value.status == B.EPARA_ERR_SHAPE and np.array_equal(refs, before[0]) and pool.n_free == before[1]
+            continue
+        child, move = B.epara_pages_fork(pool, left, tokens)
+        want, moves = ref.fork(left, tokens)
+        assert child.tolist() == want and [tuple(m) for m in move.tolist()] == moves and child[:2].tolist() == [-1, -1]
+        assert refs.tolist() == ref.refs and free[: pool.n_free].tolist() == ref.free_pages
+        B.epara_pages_free(pool, child)
+        ref.free(want)
+    for bad in (-2, 8, int(free[0])):
+        with pytest.raises(B.EparaError):
+            B.epara_pages_fork(pool, [bad] + left[1:], 256)
