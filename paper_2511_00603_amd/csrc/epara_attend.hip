@@ -104,6 +104,7 @@ __device__ __forceinline__ work_item find_work(const epara_cache_attn_args* __re
     const int i = find_sequence(first, n_seqs, item, lane);
     w.s = seqs[i];
     w.a = args[w.s.service];
+    w.a.window = min_of(w.a.window, EPARA_CACHE_MAX_TOKENS);        // no more tokens are there, and positions less a window stay in 32 bits
     w.group = w.a.heads / w.a.kv_heads;
     w.rows = w.s.rows * w.group;
     const int tiles = (w.rows + SIZE - 1) / SIZE, local = item - first[i];

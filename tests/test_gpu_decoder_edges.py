@@ -6,7 +6,7 @@ import torch
 
 from oracle import decoder as OD
 from paper_2511_00603_amd import runtime as R
-from test_gpu_decoder import BF, DEV, SLACK, Case, check_attn, dev_bf16, fetch, run_attn, sync
+from test_gpu_decoder import BF, DEV, SLACK, Case, attn_case, check_attn, dev_bf16, fetch, run_attn, sync
 
 pytestmark = pytest.mark.gpu
 
@@ -166,3 +166,12 @@ def test_rmsnorm_of_rows_of_any_size(kind, eps, with_r):
             assert (np.abs(scale - least) <= 1e-6 * least).all()
         got, limit = OD.e4m3_decode(g["Y"].cpu().numpy()) * scale, np.clip(y, -448 * scale, 448 * scale)
         assert (np.abs(got - limit) <= np.maximum(np.abs(limit) * 2.0 ** -4, scale * 2.0 ** -10) * SLACK).all()
+
+
+@pytest.mark.parametrize("window", [2**24, 2**31 - 1])
+def test_attention_with_windows_wider_than_any_sequence(window):
+    """Positions less such a window would pass 32 bits; rows of padding next to rows that see keys, few and many."""
+    rng = np.random.default_rng([107])
+    cases = [attn_case(rng, [-5, -300, 0, 100, -2000], [7, 310, 40, 1, 2003], 4, 2, D, window, softcap) for D, softcap in ((64, 0.0), (128, 30.0))]
+    run_attn(cases)
+    check_attn(cases)
