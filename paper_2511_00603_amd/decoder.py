@@ -47,24 +47,35 @@ class DecoderBlock:
         if child in self.sequences[service]:
             raise ValueError("sequence %r exists" % (child,))
         own, moves = self.pools[service].fork(pages, tokens)
+        try:
+            self._copy(service, moves)
+        except BaseException:
+            self.pools[service].free(own)
+            raise
         self.sequences[service][child] = [own.tolist(), tokens]
-        if len(moves):
-            R.copy_pages(R.PageCopyPlan([{"cache": self.caches[service], "moves": moves}], self.device))
 
     def release(self, service, name):
         self.pools[service].free(self.sequences[service].pop(name)[0])
 
     def compact(self, service):
         """-> how many pages moved."""
-        seqs = self.sequences[service]
+        seqs, pool, at = self.sequences[service], self.pools[service], 0
         table = np.array([p for pages, _ in seqs.values() for p in pages], dtype=np.int32)
-        moves, at = self.pools[service].compact(table), 0
+        before = pool.state()
+        moves = pool.compact(table)
+        try:
+            self._copy(service, moves)
+        except BaseException:
+            pool.restore(before)
+            raise
         for s in seqs.values():
             s[0] = table[at: at + len(s[0])].tolist()
             at += len(s[0])
+        return len(moves)
+
+    def _copy(self, service, moves):
         if len(moves):
             R.copy_pages(R.PageCopyPlan([{"cache": self.caches[service], "moves": moves}], self.device))
-        return len(moves)
 
     # ---- one step
     def step(self, new):

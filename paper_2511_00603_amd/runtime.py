@@ -508,3 +508,10 @@ class PagePool:
 
     def compact(self, table):
         return B.epara_pages_compact(self.c, table)
+
+    def state(self):
+        """A copy of who holds what, for restore()."""
+        return self.refs.copy(), self.free_pages.copy(), int(self.c.n_free)
+
+    def restore(self, state):
+        self.refs[:], self.free_pages[:], self.c.n_free = state

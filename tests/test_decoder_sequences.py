@@ -66,3 +66,28 @@ def test_pages_go_back_when_something_fails_after_they_were_taken(monkeypatch):
 
     monkeypatch.setattr(DecoderBlock, "_launch", broken)
     refused(b, [[("a", X(70)), ("n", X(5))], [("b", X(100))]], RuntimeError)
+
+
+def test_a_fork_or_a_compaction_whose_copy_fails_changes_nothing(monkeypatch):
+    def broken(*_):
+        raise RuntimeError("no memory")
+
+    b = block(n_pages=10)
+    b.device, b.caches = "cpu", [None, None]
+    taken(b, [[("a", X(100)), ("b", X(64)), ("c", X(10))], []])
+    b.release(0, "b")
+    before = state(b)
+    monkeypatch.setattr(R, "PageCopyPlan", broken)
+    for f in (lambda: b.fork(0, "a", "child"), lambda: b.compact(0)):
+        with pytest.raises(RuntimeError):
+            f()
+        assert state(b) == before
+    with pytest.raises(ValueError):
+        b.fork(0, "a", "c")                                      # a name that is taken
+    assert state(b) == before
+    monkeypatch.setattr(R, "PageCopyPlan", lambda groups, device: groups)
+    copied = []
+    monkeypatch.setattr(R, "copy_pages", copied.extend)
+    b.fork(0, "a", "child")
+    b.compact(0)
+    assert [len(s[0]) for s in b.sequences[0].values()] == [2, 1, 2] and len(copied) == 1       # nothing lies above the pages in use: the child took the gap
