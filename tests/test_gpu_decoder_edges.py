@@ -175,3 +175,29 @@ def test_attention_with_windows_wider_than_any_sequence(window):
     cases = [attn_case(rng, [-5, -300, 0, 100, -2000], [7, 310, 40, 1, 2003], 4, 2, D, window, softcap) for D, softcap in ((64, 0.0), (128, 30.0))]
     run_attn(cases)
     check_attn(cases)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("window,softcap", [(2501, 0.0), (3030, 20.0), (0, 20.0)])
+def test_attention_over_cut_contexts_with_windows_and_capped_scores(D, window, softcap):
+    """Contexts in parts that begin where a window does, of few and of many rows; tiles of a sequence with different numbers of parts; the same bits every time."""
+    rng = np.random.default_rng([108, D, window])
+    c = attn_case(rng, [9000, 4097, 3000, 6000], [1, 5, 64, 200], 4, 1, D, window, softcap)
+    plan = run_attn([c])
+    check_attn([c])
+    assert plan.plan.workspace_bytes > 0
+    for few, (start, rows) in ((True, (9000, 1)), (True, (4097, 5)), (False, (3000, 64)), (False, (6000, 200))):
+        tile, part = (16, plan.plan.part_pages[0]) if few else (128, plan.plan.part_pages[1])
+        counts = set()
+        for first in range(0, 4 * rows, tile):
+            lo, hi = start + first // 4, start + (min(first + tile, 4 * rows) - 1) // 4
+            pages = hi // 64 + 1 - (max(0, lo - window + 1) // 64 if window else 0)
+            counts.add(-(-pages // part))
+        assert min(counts) > 1                                   # every sequence is cut
+        assert len(counts) > 1 or window != 3030 or rows != 200  # and tiles have different numbers of parts here
+    got = c[2]["O"].clone()
+    for _ in range(3):
+        c[2]["O"].fill_(float("nan"))
+        R.cache_attention(plan)
+        sync()
+        assert torch.equal(c[2]["O"].view(torch.int16), got.view(torch.int16))
