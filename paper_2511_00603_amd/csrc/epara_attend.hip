@@ -130,7 +130,8 @@ __device__ __forceinline__ v2f get2(const float* at)
     return v2f{__uint_as_float(static_cast<uint32_t>(v)), __uint_as_float(static_cast<uint32_t>(v >> 32))};
 }
 
-constexpr float NOTHING = -1e30f;                          // reference of a row that has seen no key
+constexpr float NOTHING = -3e38f;                          // reference of a row that has seen no key
+constexpr float LARGE = 4096.f;                            // references from which on a score is rounded before M is taken from it
 constexpr float ABOVE = 6.f, LIFT = 9.f;                   // a weight is at most 2^(ABOVE + LIFT) = 2^15
 constexpr float MOST = 32768.f;                            // sum of weights in which none can be more than that
 constexpr float FAR = 4000.f;                              // farther than any two scales
@@ -154,6 +155,18 @@ __device__ __forceinline__ float raise_references(row_state& s, float top, float
     s.scale = scale;
     s.sum *= __builtin_amdgcn_exp2f(gone);
     return f;
+}
+
+// Exponent of a weight, z unit - M + (LIFT + shift).  In one operation, which keeps the product's bits beyond fp32, as long as M is small: they are under 2^-12 then.
+// For large scores they would tell equal ones apart, up to 2^x where M is of 2^(x + 24), and what is added to M would be lost in it: the product is
+// rounded as the one that M comes from, and M taken off first.
+template <bool V> struct flag { static constexpr bool value = V; };
+__device__ __forceinline__ bool is_large(float ref) { return __ballot(fabsf(ref) > LARGE && ref != NOTHING) != 0; }
+__device__ __forceinline__ float large_exponent(float z, float unit, float ref, float more)
+{
+#pragma clang fp contract(off)
+    const float score = z * unit;
+    return score - ref + more;
 }
 
 // The scales of a page and head: keys' and values' exponents of both blocks.  A block behind the last token has whatever the memory holds.
@@ -391,6 +404,7 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
     page_list list = pages_of(w, pages, lane);
 
     row_state state = {NOTHING, NO_SCALE, 0.f};
+    bool large = false;                                    // some row's scores are
     v4f o[D / 16];
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) o[d] = v4f{0.f, 0.f, 0.f, 0.f};
@@ -463,17 +477,29 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
             float top = fmaxf(mine, __shfl_xor(mine, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
             const float f = raise_references<16, 32>(state, top, mine, exponent);
+            large = is_large(state.ref);
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) o[d] *= f;
         }
         const int shift = max_of(exponent - state.scale, LEAST_SHIFT);      // my block's scale against V
-        const float lift = LIFT - state.ref + static_cast<float>(shift);
+        const float on_top = LIFT + static_cast<float>(shift), lift = on_top - state.ref;
+        if (large) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[t][i] = large_exponent(z[t][i], unit, state.ref, on_top);
+        } else {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[t][i] = fmaf(z[t][i], unit, lift);
+        }
         float sum = 0.f, weight[16];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                weight[4 * t + i] = __builtin_amdgcn_exp2f(fmaf(z[t][i], unit, lift));
+                weight[4 * t + i] = __builtin_amdgcn_exp2f(z[t][i]);
                 sum += weight[4 * t + i];
             }
         state.sum += __builtin_ldexpf(sum, -shift);
@@ -643,6 +669,7 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
     };
 
     row_state state = {NOTHING, NO_SCALE, 0.f};
+    float most = MOST;                                     // of a sum; -1 where some row's scores are large, so that every sum is looked at
     v16f o[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -732,13 +759,13 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
         // ---- weights of a tile, and their sum with and without (`plain`) the values' scale (in fp32 before they are rounded: a block of small values may leave f16
         // nothing of its weights, but the sum needs them).  The references are raised only where the sum says that a weight may have left f16's range: no
         // maximum is formed otherwise.  The first page's weights are infinite against NOTHING.
-        auto weigh = [&](int u, v8h* weights, float& plain) -> float {
+        auto weigh = [&](int u, v8h* weights, float& plain, auto careful) -> float {
             const int shift = max_of(ps.value[u] - state.scale, LEAST_SHIFT);
-            const float lift = LIFT - state.ref + static_cast<float>(shift);
+            const float on_top = LIFT + static_cast<float>(shift), lift = on_top - state.ref;
             float x[16], sum[2] = {0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                x[i] = __builtin_amdgcn_exp2f(fmaf(z[u][i], unit[u], lift));
+                x[i] = __builtin_amdgcn_exp2f(careful.value ? large_exponent(z[u][i], unit[u], state.ref, on_top) : fmaf(z[u][i], unit[u], lift));
                 sum[i & 1] += x[i];
             }
             weights[0] = narrow(x);
@@ -753,6 +780,7 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
             top *= unit[u];
             top = fmaxf(top, __shfl_xor(top, 32));         // the other half of the row
             scale_sums(raise_references<>(state, top, top, ps.value[u]));
+            most = is_large(state.ref) ? -1.f : MOST;
         };
         auto add_values = [&](int u, const v8h* weights) {
 #pragma unroll
@@ -762,18 +790,17 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
                     o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds8h(here + VALUES + ((d * 2 + u) * 2 + j) * 1024), weights[j], o[d], 0, 0, 0);
         };
         v8h first[2], second[2];
-        float plain;
-        if (__ballot(weigh(0, first, plain) > MOST)) {
-            raise(0);
-            weigh(0, first, plain);
-        }
-        state.sum += plain;
+        auto settle = [&](int u, v8h* weights) {           // one branch, seldom taken: to raise the references, and for large scores
+            float plain;
+            if (__ballot(weigh(u, weights, plain, flag<false>()) > most)) {
+                raise(u);                                  // (references that need not rise stay)
+                weigh(u, weights, plain, flag<true>());
+            }
+            state.sum += plain;
+        };
+        settle(0, first);
         add_values(0, first);
-        if (__ballot(weigh(1, second, plain) > MOST)) {
-            raise(1);
-            weigh(1, second, plain);
-        }
-        state.sum += plain;
+        settle(1, second);
         add_values(1, second);
         swap();
         next = later;

@@ -201,3 +201,24 @@ def test_attention_over_cut_contexts_with_windows_and_capped_scores(D, window, s
         R.cache_attention(plan)
         sync()
         assert torch.equal(c[2]["O"].view(torch.int16), got.view(torch.int16))
+
+
+@pytest.mark.parametrize("rows", [1, 90])
+@pytest.mark.parametrize("power", [10, 20, 24, 28, 34, 60, 100])
+def test_attention_with_scores_that_leave_fp32_no_fractions(rows, power):
+    """Scores of up to 2^power whose differences are as large (each one exact up to the factor log2 e, alike for equal keys): all the weight lies on the largest, shared alike by the keys
+    that have it, in blocks of different scales."""
+    for D in (64, 128):
+        n, rng = 330, np.random.default_rng([109, rows, D])
+        K, V = np.zeros((n, 1, D)), rng.standard_normal((n, 1, D)) * np.exp2(np.repeat(rng.integers(-12, 12, 11), 32))[:n, None, None]
+        K[:, 0, 0] = -rng.integers(1, 8, n)
+        K[rng.choice(n - rows, 6 if rows < 90 else 40, replace=False), 0, 0] = rng.choice([7.0, 6.0])
+        q = np.zeros((rows, 2 * D))
+        q[:, 0], q[:, D] = 1.0, -1.0
+        c = one_sequence(rng, n, rows, D, K, V, q)
+        c[2]["scale"] = 2.0 ** (power - 3)
+        run_attn([c])
+        got = fetch(c[2]["O"]).reshape(rows, 2, D)
+        keys, values = c[0].oracle.values(c[1][0]["pages"], n)
+        want, mass = OD.attention(c[3], keys, values, n - rows, 2.0 ** (power - 3))
+        assert (np.abs(got - want) <= (2.0 ** -8 + 2.0 ** -10) * mass + BF * np.abs(want)).all()
