@@ -973,7 +973,8 @@ typedef struct {
     const epara_cache_attn_args* d_args;
     const int32_t* h_first;     /* int32[2 * (n_seqs + 1)] */
     const int32_t* d_first;
-    void*   d_workspace;        /* 256-byte aligned, zeroed once (epara_workspace_init) before its first call; one call at a time */
+    void*   d_workspace;        /* 256-byte aligned; one call at a time.  Zeroed (epara_workspace_init) before the first call of a plan, and again after calls
+                                   of another plan have used it: they leave sums where this one counts; its own calls leave the counts at zero */
     int64_t workspace_bytes;
     epara_sequence_table table;
     epara_cache_attn_plan plan;

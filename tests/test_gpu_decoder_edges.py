@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from oracle import decoder as OD
+from paper_2511_00603_amd import binding as B
 from paper_2511_00603_amd import runtime as R
 from test_gpu_decoder import BF, DEV, SLACK, Case, attn_case, check_attn, dev_bf16, fetch, run_attn, sync
 
@@ -222,3 +223,23 @@ def test_attention_with_scores_that_leave_fp32_no_fractions(rows, power):
         keys, values = c[0].oracle.values(c[1][0]["pages"], n)
         want, mass = OD.attention(c[3], keys, values, n - rows, 2.0 ** (power - 3))
         assert (np.abs(got - want) <= (2.0 ** -8 + 2.0 ** -10) * mass + BF * np.abs(want)).all()
+
+
+def test_attention_plans_that_share_a_workspace():
+    """Two plans with different numbers of workgroups take turns on one workspace, zeroed whenever the plan changes; a plan's own calls need nothing in between."""
+    rng = np.random.default_rng(110)
+    cases = [attn_case(rng, starts, news, 4, 2, 128) for starts, news in (([9000], [1]), ([3000] * 9, [2, 60, 1, 1, 90, 1, 1, 1, 1]))]
+    plans = [R.CacheAttnPlan(R.SequenceTable([c[1]], DEV), [c[2]], DEV) for c in cases]
+    size = max(p.plan.workspace_bytes for p in plans)
+    shared = torch.full((size,), 0xFF, dtype=torch.uint8, device=DEV)
+    for p in plans:
+        assert p.plan.workspace_bytes > 0
+        p.c.d_workspace, p.c.workspace_bytes = shared.data_ptr(), size
+    for _ in range(2):
+        for c, p in zip(cases, plans):
+            B.epara_workspace_init(shared.data_ptr(), -(-4 * sum(p.plan.n_items) // 256) * 256, R.current_stream_handle())
+            for _ in range(2):
+                c[2]["O"].fill_(float("nan"))
+                R.cache_attention(p)
+                sync()
+                check_attn([c])
