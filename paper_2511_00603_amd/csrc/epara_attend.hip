@@ -26,11 +26,11 @@
 //   many rows (a tile of 128, 32 to a wave): 32x32x16.  Lane (n = lane % 32, h = lane / 32) gets from the two tiles u of S^T of a page the scores of row n
 //     with the keys 32 u + 16 h + 0 .. 15, again a chunk.  Pages go through the registers, where they are widened once for all four waves, to the LDS.
 //
-// Few rows are bound by HBM: a token of 105 requests (0.42 GB of cache) 79 us, 5.4 TB/s; of 16 requests at 16384 tokens 86 us, 6.2 TB/s; of one at 32768
-// 20 us, of which 8 are start, joining and launch.  The pages of a wave are 16 KiB in whole lines; two waves per SIMD have 128 KiB in flight in a compute unit.
-// They are read with the non-temporal hint, since a model's layers together pass any cache (without it 89 and 98 us; one request the same).
-// Many rows are bound by no single unit: two prompts of 4096 tokens 281 us, 980 TFLOP/s, with the matrix cores busy 43 % of the time, the
-// LDS 33 %; two workgroups of a compute unit wait on barriers and the LDS in turn.  Widening once for all four waves instead of in each: 314 us before.
+// Few rows are bound by HBM: a token of 105 requests (0.42 GB of cache) 77 us, 5.5 TB/s; of 16 requests at 16384 tokens 87 us, 6.2 TB/s; of one at 32768
+// 19.4 us, of which 7 are start, joining and launch.  The pages of a wave are 16 KiB in whole lines; two waves per SIMD have 128 KiB in flight in a compute unit.
+// They are read with the non-temporal hint, since a model's layers together pass any cache (without it 86 and 98 us; one request the same).
+// Many rows are bound by no single unit: two prompts of 4096 tokens 274 us, 1000 TFLOP/s, with the matrix cores busy 46 % of the time, the
+// LDS 35 %; two workgroups of a compute unit wait on barriers and the LDS in turn.  Widening once for all four waves instead of in each took 314 us to 291.
 // (The results of the matrix instructions are never read by an inline instruction: the compiler puts the waits they need only in front of its own.)
 #include <hip/hip_runtime.h>
 #include <math.h>

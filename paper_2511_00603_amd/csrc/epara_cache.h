@@ -51,7 +51,8 @@ EPARA_BOTH int64_t append_items(const epara_append_args& a, const append_shape& 
 // token; a workgroup takes a tile of them against a part of the pages that the tile sees.
 constexpr int FEW_TILE = 16, MANY_TILE = 128;
 // Up to 32 rows to a key head are few.  Two tiles of 16 read a page twice, the second time from a die's cache, where a tile of 128 would leave three
-// waves idle: 2 requests with 32 rows at 8000 tokens 16 us against 34, 16 of them 59 against 56; 64 rows 21 against 38 and 118 against 71.
+// waves idle: 2 requests with 32 rows at 8000 tokens 16 us against 30, 16 of them 60 against 56; 64 rows 20 against 32 and 101 against 69.  (One limit for
+// all loads: what is better at 32 to 64 rows depends on how many requests there are.)
 constexpr int FEW_MAX_ROWS = 32;
 constexpr int MAX_PARTS = 128;                             // of a tile's pages
 constexpr int SLOT_FLOATS = 128 + 4;                       // per row of a part: the weighted sum of values, both references and the sum of weights

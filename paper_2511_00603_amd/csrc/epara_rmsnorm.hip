@@ -6,7 +6,7 @@
 // maximum of |s gamma| are reduced together, since max |y| = max |s gamma| / sqrt(..).  A row whose squares leave fp32's range (values from 2^57 on, or
 // all under 2^-48 with an eps no larger than their squares) is taken once more, from the registers, with its power of two taken out.
 // Bound by HBM: 8192 rows of 5120 in bf16 64 us (5.2 TB/s), in 8 bits with a scale per row 57 us (5.1 TB/s); with a wave per row, whose 80 chunks
-// leave room for one wave per SIMD, 96 and 91.  105 rows of 4096 (a launch and its trips to memory) 3.5 us alone, 6.1 with a wave per row.
+// left room for one wave per SIMD, 96 and 91.  105 rows of 4096 (a launch and its trips to memory) 3.5 us alone, 6.1 with a wave per row.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
