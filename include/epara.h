@@ -1012,6 +1012,123 @@ typedef struct {
 int32_t epara_copy_pages(const epara_page_copy* h_caches, const epara_page_copy* d_caches, int32_t G,
                          const epara_page_move* h_moves, const epara_page_move* d_moves, int32_t n_moves, void* stream);
 
+/* ---- device side: decoding by drafts -------------------------------------------------------- */
+
+/* A service may try several tokens of a sequence at once: a step takes the last token that is certain and tokens that somebody has guessed (drafted)
+ * behind it, as a chain or as a tree of alternatives, through the model as new rows of the sequence; those that the model itself agrees to stay, and
+ * the others leave the cache.  Per step and for all services at once:
+ *   epara_draft_trees     which rows each row follows, and its rotary position, from the rows' parents;
+ *   epara_cache_append    with these positions: row i of a sequence lies at slot start + i of its pages, whatever its position;
+ *   epara_tree_attention  in place of epara_cache_attention;
+ *   epara_verify_drafts   on the rows' logits: which rows stay, and the next token;
+ *   epara_cache_keep      closes up the rows that stay in the caches of all layers: the sequence then has start + kept tokens.
+ * None of them allocates or synchronises, and all read what the one before has written on the device, so that a step can be captured once. */
+#define EPARA_TREE_MAX_ROWS 256
+
+/* One service's drafts.  Rows are those of its tensors; a parent names a row counted from its sequence's first.  -1: the row follows the tokens
+ * before the call.  A row whose parent is anything but -1 or an earlier row is not there, and neither is a row that follows it: it sees nothing, nothing sees
+ * it, it never stays (so that a captured step can take trees of different sizes).  A sequence of more than EPARA_TREE_MAX_ROWS rows is no tree:
+ * its parents are not read, and each of its rows follows the one before.  32 bytes, the same on host and device. */
+typedef struct {
+    const int32_t* parents;     /* device, int32 [rows] (epara_draft_trees alone reads them) */
+    uint64_t*      visible;     /* device, uint64 [rows, 4], 16-byte aligned: bit j % 64 of word j / 64: the row follows row j of its sequence, or is it; all 0: it is not there */
+    int32_t*       positions;   /* device, int32 [rows, 3], or NULL: start + how many rows it follows, on all three axes (start for a row that is not there) */
+    int32_t        rows;
+    int32_t        reserved;
+} epara_tree_args;
+
+/* Writes visible and positions of the rows of all sequences; visible of sequences that are no trees is left as it is.  One kernel, a workgroup to a sequence.
+ * Errors: ERR_NULL; ERR_SHAPE (rows < 0, a sequence outside its service's rows or its pages, a row of two sequences, a tree that starts before position 0);
+ * ERR_ALIGN; ERR_CAPACITY (no host memory). */
+int32_t epara_draft_trees(const epara_tree_args* h_args, const epara_tree_args* d_args, int32_t G, const epara_sequence_table* table, void* stream);
+
+/* epara_cache_attention for sequences whose new rows are trees: with d(i) the number of rows that row i of a sequence follows, it is at position start + d(i) and sees
+ * the tokens 0 .. start - 1 (window: those > start + d(i) - window), the rows that it follows, and itself.  A row that is not there gets zeros.  The arithmetic is
+ * epara_cache_attention's; workspace, launch and errors too.  trees[g].visible NULL: that service's sequences are no trees (causal, as in
+ * epara_cache_attention), and so are sequences of more than EPARA_TREE_MAX_ROWS rows.  parents and positions are not looked at.
+ * Also ERR_SHAPE: a tree that starts before position 0, or has more rows than a window; trees[g].rows other than the service's. */
+int32_t epara_plan_tree_attention(const epara_cache_attn_args* h_args, const epara_tree_args* h_trees, int32_t G, const epara_sequence_table* table, int32_t n_compute_units,
+                                  int32_t* first, epara_cache_attn_plan* plan);
+int32_t epara_tree_attention(const epara_cache_attn_launch* launch, const epara_tree_args* h_trees, const epara_tree_args* d_trees, void* stream);
+
+/* One service's part of epara_verify_drafts.  72 bytes. */
+typedef struct {
+    const void*    logits;        /* device, the call's dtype, row r at logits + r * stride elements: the target's, of the token behind row r */
+    const void*    draft_logits;  /* the same type, row r at draft_logits + r * draft_stride: what the row's first child was drawn from; NULL: tokens are given, not drawn */
+    const int32_t* tokens;        /* device, int32 [rows]: the token of each row */
+    const int32_t* parents;       /* device, int32 [rows], as above; NULL: every sequence is a chain */
+    const float*   uniforms;      /* device, fp32 [rows], from [0, 1): row r's decides about row r; the one of a sequence's first row draws the next token */
+    int32_t*       path;          /* device, int32 [rows], out: the rows that stay, in order, counted from the sequence's first; -1 behind them */
+    float*         probs;         /* device, fp32 [rows], out, or NULL: the target's probability of the row's token behind its parent; 0 for a row without a parent among the rows before it */
+    int32_t rows, vocab;
+    int32_t stride, draft_stride; /* >= vocab */
+} epara_verify_args;
+
+/* How a call is cut into work: made by epara_plan_verify_drafts.  first[0 .. n_seqs] and first[n_seqs + 1 .. 2 n_seqs + 1] are running sums of the workgroups of the
+ * sequences that read the rows' logits, and that draw the next token. */
+typedef struct {
+    int32_t n_items[2];
+    int32_t pieces;               /* a workgroup takes 256 * pieces pieces of 16 bytes of a row: 1, 2, 4 or 8 */
+    int32_t reserved;
+    int64_t workspace_bytes;
+} epara_verify_plan;
+
+typedef struct {
+    const epara_verify_args* h_args;
+    const epara_verify_args* d_args;
+    const int32_t* h_first;       /* int32[2 * (n_seqs + 1)] */
+    const int32_t* d_first;
+    const float* d_temperatures;  /* device, fp32 [n_seqs]; NULL: all 0 */
+    int32_t*     d_kept;          /* device, int32 [n_seqs], out: rows that stay, the first among them; 0 for a sequence without rows */
+    int32_t*     d_next;          /* device, int32 [n_seqs], out: the token behind the last of them; -1 without one */
+    void*        d_workspace;     /* 256-byte aligned; one call at a time.  Its first 4 * n_seqs bytes are zeroed (epara_workspace_init) before the first call of a plan, and again
+                                     after calls of another plan have used it; its own calls leave them at zero */
+    int64_t      workspace_bytes;
+    epara_sequence_table table;   /* of a sequence only service, first_row and rows (at most EPARA_TREE_MAX_ROWS) are looked at */
+    epara_verify_plan plan;
+    int32_t      G, dtype;        /* EPARA_BF16 or EPARA_F32 */
+} epara_verify_launch;
+
+/* Which drafts stay, and the token behind them, so that tokens come out as if the target had drawn each of them itself (speculative sampling: Leviathan et al. 2023,
+ * Chen et al. 2023; trees of given tokens: each is tried against what its elder siblings have left).  p_r = softmax(logits_r / T) with the sequence's
+ * temperature T (held to [2^-100, 2^100]); T <= 0 (or a NaN): p_r is 1 at the largest logit (the lowest of equal ones).  A sequence's first row stays.  From the row r that stays last:
+ *   tokens are given:  its children in order, with M = 1 at first: a child c whose token x is a token of the vocabulary that no elder sibling has stays if u_c M < p_r(x);
+ *                      otherwise M loses p_r(x) and the next child is tried;
+ *   tokens are drawn:  its first child c alone: it stays if u_c q_r(x) < p_r(x), with q_r = softmax(draft_logits_r / T).  (With T <= 0 as above.)
+ * Behind the last one that stays, the next token is the first v with sum_{i <= v} w_i > u sum_i w_i, where w is p_r without the tokens of its children
+ * (given), max(p_r - q_r, 0) if it has a child with a token of the vocabulary (drawn), or p_r.  Where all of w is 0 it is the one with the largest logit.
+ * A row whose logits have a NaN, +infinity or nothing above -infinity has no distribution: no child of it stays, the next token behind it is -1, probabilities are 0; drafts' logits of
+ * that kind: the child does not stay and the next token is drawn from p_r.  Uniforms below 0 and NaN count as 0, those from 1 on as the largest number below.
+ * Sums and probabilities that decide about drafts are fp32 products summed in fp64; the next token's weights and sums are fp64 throughout, since the borders between tokens lie close.
+ * Logits of every row are read once, draft logits of rows with a child once, and those of the row behind which a token is drawn again.
+ * Errors: ERR_NULL; ERR_DTYPE; ERR_SHAPE (a dimension out of range, a sequence of too many rows or outside the service's, a row of two sequences, h_first not the plan's); ERR_ALIGN (pointers
+ * not a multiple of their elements' size, workspace); ERR_CAPACITY (workspace, too much work for one grid, or no host memory). */
+int32_t epara_plan_verify_drafts(const epara_verify_args* h_args, int32_t G, const epara_sequence_table* table, int32_t dtype, int32_t n_compute_units,
+                                 int32_t* first, epara_verify_plan* plan);
+int32_t epara_verify_drafts(const epara_verify_launch* launch, void* stream);
+
+/* The cache of one layer in epara_cache_keep; the layers of a service share their path.  56 bytes. */
+typedef struct {
+    void*          codes;
+    uint8_t*       scales;
+    const int32_t* path;          /* device, int32 [rows], as epara_verify_drafts writes it */
+    int32_t service;              /* whose sequences */
+    int32_t first_seq;            /* the service's first sequence in the table (where it would be, if it has none) */
+    int32_t rows;                 /* of the service */
+    int32_t n_pages, kv_heads, head_dim;
+    int32_t first_item;           /* running sum over the earlier caches of (sequences of the service in the table) * kv_heads */
+    int32_t reserved;
+} epara_keep_args;
+
+/* The rows that stay move together: for each sequence, token start + path[i] of its pages becomes token start + i, for i < d_kept[its index in the table].  A block of 32 tokens
+ * that gets any takes the largest of the exponents that its tokens (earlier ones too) have; codes are rescaled, and rounded again, only where that is more than they had.  What else lies
+ * in the pages is left as it is.  A path that does not rise, or leaves the sequence's rows, ends there; kept is held to 0 .. rows.  Nothing moves in a sequence of more than
+ * EPARA_TREE_MAX_ROWS rows.  One kernel, a wave to a cache, sequence and head.
+ * Errors: ERR_NULL; ERR_SHAPE (a dimension out of range, rows outside the service's, a tree that starts before position 0, a page outside the cache or under new rows of two
+ * sequences of one cache, a cache twice, first_seq or first_item not the table's); ERR_ALIGN; ERR_CAPACITY (too much work for one grid, or no host memory). */
+int32_t epara_cache_keep(const epara_keep_args* h_caches, const epara_keep_args* d_caches, int32_t n_caches, const epara_sequence_table* table,
+                         const int32_t* d_kept, void* stream);
+
 /* ---- host side: which page belongs to whom -------------------------------------------------- */
 
 /* The pages of a cache and how many sequences hold each.  The caller owns both arrays. */

@@ -51,9 +51,16 @@ CACHE_ATTN_ARGS = np.dtype([("Q", "<u8"), ("O", "<u8"), ("codes", "<u8"), ("scal
 PAGE_MOVE = np.dtype([("src", "<i4"), ("dst", "<i4")])
 PAGE_COPY = np.dtype([("codes", "<u8"), ("scales", "<u8"), ("n_pages", "<i4"), ("kv_heads", "<i4"), ("head_dim", "<i4"),
                       ("first_move", "<i4"), ("n_moves", "<i4"), ("first_chunk", "<i4")])
+TREE_ARGS = np.dtype([("parents", "<u8"), ("visible", "<u8"), ("positions", "<u8"), ("rows", "<i4"), ("reserved", "<i4")])
+VERIFY_ARGS = np.dtype([("logits", "<u8"), ("draft_logits", "<u8"), ("tokens", "<u8"), ("parents", "<u8"), ("uniforms", "<u8"), ("path", "<u8"), ("probs", "<u8"),
+                        ("rows", "<i4"), ("vocab", "<i4"), ("stride", "<i4"), ("draft_stride", "<i4")])
+KEEP_ARGS = np.dtype([("codes", "<u8"), ("scales", "<u8"), ("path", "<u8"), ("service", "<i4"), ("first_seq", "<i4"), ("rows", "<i4"), ("n_pages", "<i4"),
+                      ("kv_heads", "<i4"), ("head_dim", "<i4"), ("first_item", "<i4"), ("reserved", "<i4")])
+assert TREE_ARGS.itemsize == 32 and VERIFY_ARGS.itemsize == 72 and KEEP_ARGS.itemsize == 56
 assert RMSNORM_ARGS.itemsize == 72 and SEQUENCE.itemsize == 24 and APPEND_ARGS.itemsize == 88 and CACHE_ATTN_ARGS.itemsize == 80
 assert PAGE_MOVE.itemsize == 8 and PAGE_COPY.itemsize == 40
 EPARA_CACHE_PAGE, EPARA_CACHE_BLOCK, EPARA_CACHE_MAX_GROUP, EPARA_CACHE_MAX_TOKENS = 64, 32, 64, 16777216
+EPARA_TREE_MAX_ROWS = 256
 EPARA_TABLE_BLOCK = 2
 SIM_REQUEST = np.dtype([("arrival_us", "<i8"), ("slo_us", "<i8"), ("service", "<i4"), ("origin", "<i4"), ("frames", "<i4"), ("fps_milli", "<i4")])
 assert SIM_REQUEST.itemsize == 32
@@ -111,6 +118,18 @@ class CacheAttnLaunch(ctypes.Structure):
     _fields_ = [("h_args", ctypes.c_void_p), ("d_args", ctypes.c_void_p), ("h_first", ctypes.c_void_p), ("d_first", ctypes.c_void_p),
                 ("d_workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64), ("table", SequenceTable), ("plan", CacheAttnPlan),
                 ("G", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class VerifyPlan(ctypes.Structure):
+    """struct epara_verify_plan."""
+    _fields_ = [("n_items", ctypes.c_int32 * 2), ("pieces", ctypes.c_int32), ("reserved", ctypes.c_int32), ("workspace_bytes", ctypes.c_int64)]
+
+
+class VerifyLaunch(ctypes.Structure):
+    """struct epara_verify_launch."""
+    _fields_ = [("h_args", ctypes.c_void_p), ("d_args", ctypes.c_void_p), ("h_first", ctypes.c_void_p), ("d_first", ctypes.c_void_p),
+                ("d_temperatures", ctypes.c_void_p), ("d_kept", ctypes.c_void_p), ("d_next", ctypes.c_void_p), ("d_workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_int64), ("table", SequenceTable), ("plan", VerifyPlan), ("G", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
 class PagePool(ctypes.Structure):
@@ -262,6 +281,14 @@ def lib():
         L.epara_pages_fork.argtypes = [vp, vp, i32, vp, vp, vp]
         L.epara_pages_free.argtypes = [vp, vp, i32]
         L.epara_pages_compact.argtypes = [vp, vp, i32, vp, i32, vp]
+        L.epara_draft_trees.argtypes = [vp, vp, i32, vp, vp]
+        L.epara_plan_tree_attention.argtypes = [vp, vp, i32, vp, i32, vp, vp]
+        L.epara_tree_attention.argtypes = [vp, vp, vp, vp]
+        L.epara_plan_verify_drafts.argtypes = [vp, i32, vp, i32, i32, vp, vp]
+        L.epara_verify_drafts.argtypes = [vp, vp]
+        L.epara_cache_keep.argtypes = [vp, vp, i32, vp, vp, vp]
+        for name in ("epara_draft_trees", "epara_plan_tree_attention", "epara_tree_attention", "epara_plan_verify_drafts", "epara_verify_drafts", "epara_cache_keep"):
+            getattr(L, name).restype = i32
         for name in ("epara_add_rmsnorm", "epara_plan_cache_append", "epara_cache_append", "epara_plan_cache_attention", "epara_cache_attention",
                      "epara_copy_pages", "epara_page_pool_init", "epara_pages_take", "epara_pages_fork", "epara_pages_free", "epara_pages_compact"):
             getattr(L, name).restype = i32
@@ -400,6 +427,50 @@ def epara_copy_pages(h_caches, d_caches, h_moves, d_moves, stream=0):
     h_caches, h_moves = np.ascontiguousarray(h_caches, dtype=PAGE_COPY), np.ascontiguousarray(h_moves, dtype=PAGE_MOVE)
     _check(lib().epara_copy_pages(_ptr(h_caches) if len(h_caches) else None, int(d_caches) or None, len(h_caches),
                                   _ptr(h_moves) if len(h_moves) else None, int(d_moves) or None, len(h_moves), int(stream) or None), "epara_copy_pages")
+
+
+def epara_draft_trees(h_args, d_args, table, stream=0):
+    """h_args: TREE_ARGS[G] (host copy, validated); d_args: device address of the same bytes; table: a SequenceTable."""
+    h_args = np.ascontiguousarray(h_args, dtype=TREE_ARGS)
+    _check(lib().epara_draft_trees(_ptr(h_args) if len(h_args) else None, int(d_args) or None, len(h_args), ctypes.addressof(table), int(stream) or None), "epara_draft_trees")
+
+
+def epara_plan_tree_attention(h_args, h_trees, table, n_compute_units):
+    """h_args: CACHE_ATTN_ARGS[G], h_trees: TREE_ARGS[G] -> (running sums int32[2 (n_seqs + 1)], CacheAttnPlan)."""
+    h_args, h_trees = np.ascontiguousarray(h_args, dtype=CACHE_ATTN_ARGS), np.ascontiguousarray(h_trees, dtype=TREE_ARGS)
+    if len(h_args) != len(h_trees):
+        raise ValueError("%d services, trees of %d" % (len(h_args), len(h_trees)))
+    first, plan = np.zeros(2 * (table.n_seqs + 1), dtype=np.int32), CacheAttnPlan()
+    _check(lib().epara_plan_tree_attention(_ptr(h_args) if len(h_args) else None, _ptr(h_trees) if len(h_trees) else None, len(h_args), ctypes.addressof(table),
+                                           int(n_compute_units), _ptr(first), ctypes.addressof(plan)), "epara_plan_tree_attention")
+    return first, plan
+
+
+def epara_tree_attention(launch, h_trees, d_trees, stream=0):
+    """launch: a CacheAttnLaunch, h_trees: TREE_ARGS[G] (kept alive, with what they point to, by the caller); d_trees: device address of the same bytes."""
+    h_trees = np.ascontiguousarray(h_trees, dtype=TREE_ARGS)
+    _check(lib().epara_tree_attention(ctypes.addressof(launch), _ptr(h_trees) if len(h_trees) else None, int(d_trees) or None, int(stream) or None), "epara_tree_attention")
+
+
+def epara_plan_verify_drafts(h_args, table, dtype, n_compute_units):
+    """h_args: VERIFY_ARGS[G] -> (running sums int32[2 (n_seqs + 1)], VerifyPlan)."""
+    h_args = np.ascontiguousarray(h_args, dtype=VERIFY_ARGS)
+    first, plan = np.zeros(2 * (table.n_seqs + 1), dtype=np.int32), VerifyPlan()
+    _check(lib().epara_plan_verify_drafts(_ptr(h_args) if len(h_args) else None, len(h_args), ctypes.addressof(table), int(dtype), int(n_compute_units),
+                                          _ptr(first), ctypes.addressof(plan)), "epara_plan_verify_drafts")
+    return first, plan
+
+
+def epara_verify_drafts(launch, stream=0):
+    """launch: a VerifyLaunch (kept alive, with what it points to, by the caller)."""
+    _check(lib().epara_verify_drafts(ctypes.addressof(launch), int(stream) or None), "epara_verify_drafts")
+
+
+def epara_cache_keep(h_caches, d_caches, table, d_kept, stream=0):
+    """h_caches: KEEP_ARGS[n] (host copy, validated); d_caches: device address of the same bytes; d_kept: device int32[n_seqs]."""
+    h_caches = np.ascontiguousarray(h_caches, dtype=KEEP_ARGS)
+    _check(lib().epara_cache_keep(_ptr(h_caches) if len(h_caches) else None, int(d_caches) or None, len(h_caches), ctypes.addressof(table), int(d_kept) or None,
+                                  int(stream) or None), "epara_cache_keep")
 
 
 def epara_page_pool_init(refs, free_pages):

@@ -1,4 +1,4 @@
-// libepara: causal attention of new tokens over a paged cache in 8 bits (the decode and prefill services' attention).
+// libepara: attention of new tokens over a paged cache in 8 bits, causal or for trees of drafted tokens (the decode and prefill services' attention).
 //
 //   o = sum_j exp(z_j - m) v_j / sum_j exp(z_j - m),   z_j = scale q . k_j (capped: c tanh(z_j / c)),   m = max_j z_j
 //
@@ -31,6 +31,8 @@
 // They are read with the non-temporal hint, since a model's layers together pass any cache (without it 86 and 98 us; one request the same).
 // Many rows are bound by no single unit: two prompts of 4096 tokens 274 us, 1000 TFLOP/s, with the matrix cores busy 46 % of the time, the
 // LDS 35 %; two workgroups of a compute unit wait on barriers and the LDS in turn.  Widening once for all four waves instead of in each took 314 us to 291.
+// A row of a tree sees the tokens before the tree and, of the tree's own, those that its 256 bits name.  Only pages that reach into the tree need them (or all, in a tile with a row
+// that is not there): a lane then shifts the page's 64 bits out of its row's.
 // (The results of the matrix instructions are never read by an inline instruction: the compiler puts the waits they need only in front of its own.)
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -94,11 +96,12 @@ struct work_item {
     int lo, hi, parts;           // the part's pages; parts of this tile
     int first_item;              // of the parts of this tile: where their counter is
     int stride;                  // from one part's item to the next
+    const uint64_t* visible;     // of the sequence's first row, or NULL: no tree
 };
 
-template <int SIZE>
-__device__ __forceinline__ work_item find_work(const epara_cache_attn_args* __restrict__ args, const epara_sequence* __restrict__ seqs,
-                                               const int32_t* __restrict__ first, int n_seqs, int part_pages, int item, int lane)
+template <int SIZE, bool TREE>
+__device__ __forceinline__ work_item find_work(const epara_cache_attn_args* __restrict__ args, const epara_tree_args* __restrict__ trees,
+                                               const epara_sequence* __restrict__ seqs, const int32_t* __restrict__ first, int n_seqs, int part_pages, int item, int lane)
 {
     work_item w;
     const int i = find_sequence(first, n_seqs, item, lane);
@@ -113,13 +116,51 @@ __device__ __forceinline__ work_item find_work(const epara_cache_attn_args* __re
     w.part = rest / tiles;
     const int back = rest - w.part * tiles;
     w.tile = tiles - 1 - back;                             // the tiles that see the most keys first
-    const page_range r = pages_of_tokens(w.s, w.a.window, w.tile * SIZE / w.group, (min_of(w.rows, w.tile * SIZE + SIZE) - 1) / w.group);
+    w.visible = TREE && is_tree(trees, w.s) ? trees[w.s.service].visible + static_cast<size_t>(w.s.first_row) * TREE_WORDS : nullptr;
+    const page_range r = pages_of_rows(w.s, w.a.window, TREE && w.visible, w.tile * SIZE / w.group, (min_of(w.rows, w.tile * SIZE + SIZE) - 1) / w.group);
     w.parts = (r.hi - r.lo + part_pages - 1) / part_pages;
     w.lo = r.lo + w.part * part_pages;
     w.hi = min_of(r.hi, w.lo + part_pages);
     w.stride = tiles * w.a.kv_heads;
     w.first_item = item - w.part * w.stride;
     return w;
+}
+
+// What a row of a tree sees: its own bits of the tree's rows, and the tokens before the tree.
+struct tree_row {
+    uint64_t bits[TREE_WORDS];
+    bool there;
+    int follows;                                           // rows
+};
+__device__ __forceinline__ tree_row tree_row_of(const work_item& w, int token)
+{
+    tree_row t;
+    const EPARA_GLOBAL v4i* src = (const EPARA_GLOBAL v4i*)(w.visible + static_cast<size_t>(token) * TREE_WORDS);
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < TREE_WORDS / 2; ++i) {
+        const v4i v = src[i];
+        t.bits[2 * i] = static_cast<uint32_t>(v[0]) | static_cast<uint64_t>(static_cast<uint32_t>(v[1])) << 32;
+        t.bits[2 * i + 1] = static_cast<uint32_t>(v[2]) | static_cast<uint64_t>(static_cast<uint32_t>(v[3])) << 32;
+        n += __builtin_popcountll(t.bits[2 * i]) + __builtin_popcountll(t.bits[2 * i + 1]);
+    }
+    t.there = n > 0;
+    t.follows = n - 1;
+    return t;
+}
+// Bit j: the row sees token `first` + j; behind: first - start, the same for all lanes.
+__device__ __forceinline__ uint64_t seen_of_page(const tree_row& t, int behind)
+{
+    if (behind <= -64) return t.there ? ~0ull : 0ull;
+    if (behind < 0) return t.there ? t.bits[0] << -behind | ((1ull << -behind) - 1) : 0ull;
+    const int word = behind >> 6, shift = behind & 63;
+    uint64_t lo = 0, hi = 0;
+#pragma unroll
+    for (int i = 0; i < TREE_WORDS; ++i) {
+        if (i == word) lo = t.bits[i];
+        if (i == word + 1) hi = t.bits[i];
+    }
+    return shift ? lo >> shift | hi << (64 - shift) : lo;
 }
 
 // 8 bytes that a workgroup on another die has written in this kernel: past the dies' own caches.  (Each lane of its own slot: a buffer's descriptor would have to be
@@ -347,7 +388,7 @@ __device__ __forceinline__ void join_few(const work_item& w, char* slots, few_ld
     }
 }
 
-template <int D>
+template <int D, bool TREE>
 __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __restrict__ pages, uint32_t* counters, char* slots, char* lds_bytes, int item)
 {
     few_lds<D>& lds = *reinterpret_cast<few_lds<D>*>(lds_bytes);
@@ -358,9 +399,17 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
 
     // ---- my row: a token and a query head
     const int row = min_of(w.tile * FEW_TILE + n, w.rows - 1), token = row / w.group, query_head = w.head * w.group + row - token * w.group;
-    const int last_key = w.s.start + token, first_key = a.window > 0 ? last_key - a.window + 1 : 0;
-    const int low_token = w.s.start + w.tile * FEW_TILE / w.group, high_token = w.s.start + (min_of(w.rows, w.tile * FEW_TILE + FEW_TILE) - 1) / w.group;
     const int end = w.s.start + w.s.rows;                  // tokens in the cache
+    const bool tree = TREE && w.visible;
+    tree_row bits = {};
+    int last_key = w.s.start + token, low_token = w.s.start + w.tile * FEW_TILE / w.group;       // pages up to low_token are seen by all rows of the tile
+    const int high_token = w.s.start + (min_of(w.rows, w.tile * FEW_TILE + FEW_TILE) - 1) / w.group;
+    if (tree) {
+        bits = tree_row_of(w, token);
+        last_key = w.s.start + bits.follows;               // its position
+        low_token = __ballot(!bits.there) ? -1 : w.s.start - 1;
+    }
+    const int first_key = a.window > 0 ? last_key - a.window + 1 : 0;
 
     // ---- the query: dims 16 q .. and (heads of 128) 64 + 16 q .., 8 to an instruction
     v8h query[KS][2];
@@ -457,13 +506,21 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
             unit = 1.f;
         }
         if (p * PAGE + PAGE - 1 > low_token || (a.window > 0 && p * PAGE <= high_token - a.window)) {
+            if (tree) {
+                const uint32_t seen = static_cast<uint32_t>(seen_of_page(bits, p * PAGE - w.s.start) >> (16 * q));
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+                for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int key = at + 4 * t + i;
-                    z[t][i] = key > last_key || key < first_key ? -INFINITY : z[t][i] * unit;
-                }
+                    for (int i = 0; i < 4; ++i) z[t][i] = !(seen >> (4 * t + i) & 1) || at + 4 * t + i < first_key ? -INFINITY : z[t][i] * unit;
+            } else {
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int key = at + 4 * t + i;
+                        z[t][i] = key > last_key || key < first_key ? -INFINITY : z[t][i] * unit;
+                    }
+            }
             unit = 1.f;
         }
         // ---- the row's largest score here: mine are 16 keys of one block, the lanes n, n + 16, .. hold the others
@@ -574,16 +631,17 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
     for (int j = 0; j < COLS; j += 4) store_out4(w, out_row, c + j, scaled4(v4f{oo[j], oo[j + 1], oo[j + 2], oo[j + 3]} * inv, static_cast<int>(vv)));
 }
 
-__global__ __launch_bounds__(NT, 2) void attend_few_kernel(const epara_cache_attn_args* __restrict__ args, const epara_sequence* __restrict__ seqs,
-                                                          const int32_t* __restrict__ pages, const int32_t* __restrict__ first, int n_seqs, int part_pages,
-                                                          uint32_t* counters, char* slots)
+template <bool TREE>
+__global__ __launch_bounds__(NT, 2) void attend_few_kernel(const epara_cache_attn_args* __restrict__ args, const epara_tree_args* __restrict__ trees,
+                                                          const epara_sequence* __restrict__ seqs, const int32_t* __restrict__ pages, const int32_t* __restrict__ first,
+                                                          int n_seqs, int part_pages, uint32_t* counters, char* slots)
 {
     __shared__ __attribute__((aligned(16))) char lds[sizeof(few_lds<128>)];
     const int item = blockIdx.x;
-    const work_item w = find_work<FEW_TILE>(args, seqs, first, n_seqs, part_pages, item, threadIdx.x & 63);
+    const work_item w = find_work<FEW_TILE, TREE>(args, trees, seqs, first, n_seqs, part_pages, item, threadIdx.x & 63);
     if (w.part > 0 && w.part >= w.parts) return;           // this tile has fewer parts than the sequence's longest
-    if (w.a.head_dim == 128) attend_few<128>(w, pages, counters, slots, lds, item);
-    else                     attend_few<64>(w, pages, counters, slots, lds, item);
+    if (w.a.head_dim == 128) attend_few<128, TREE>(w, pages, counters, slots, lds, item);
+    else                     attend_few<64, TREE>(w, pages, counters, slots, lds, item);
 }
 
 // ---- many rows -------------------------------------------------------------------------------------------------
@@ -592,7 +650,7 @@ typedef __attribute__((address_space(3))) char* ldsptr;
 __device__ __forceinline__ v8h lds8h(ldsptr at) { return *reinterpret_cast<const __attribute__((address_space(3))) v8h*>(at); }
 __device__ __forceinline__ void lds_put(ldsptr at, v8h x) { *reinterpret_cast<__attribute__((address_space(3))) v8h*>(at) = x; }
 
-template <int D>
+template <int D, bool TREE>
 __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* __restrict__ pages, uint32_t* counters, char* slots, ldsptr ring, int item)
 {
     constexpr int DT = D / 32;                             // tiles of 32 dims
@@ -604,9 +662,18 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
     const int first_row = w.tile * MANY_TILE + wave * 32;  // of my wave
     const bool live = first_row < w.rows;
     const int row = min_of(first_row + n, w.rows - 1), token = row / w.group, query_head = w.head * w.group + row - token * w.group;
-    const int last_key = w.s.start + token, first_key = a.window > 0 ? last_key - a.window + 1 : 0;
-    const int low_token = w.s.start + min_of(first_row, w.rows - 1) / w.group, high_token = w.s.start + (min_of(w.rows, first_row + 32) - 1) / w.group;
     const int end = w.s.start + w.s.rows;
+    const bool tree = TREE && w.visible;
+    tree_row bits = {};
+    int last_key = w.s.start + token, low_token = w.s.start + min_of(first_row, w.rows - 1) / w.group, lowest = low_token;      // lowest: of the rows' positions
+    const int high_token = w.s.start + (min_of(w.rows, first_row + 32) - 1) / w.group;
+    if (tree) {
+        bits = tree_row_of(w, token);
+        last_key = w.s.start + bits.follows;
+        low_token = __ballot(!bits.there) ? -1 : w.s.start - 1;
+        lowest = w.s.start;
+    }
+    const int first_key = a.window > 0 ? last_key - a.window + 1 : 0;
 
     // ---- the query: dims 32 p + 16 h .., 8 to an instruction
     constexpr int QS = D / 32;
@@ -678,7 +745,7 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
     const score_cap cap = cap_of(a, q_unit);
     // my rows see the pages [my_lo, my_hi) of the tile's; the others I only bring
     const int my_hi = live ? max_of(min_of(w.hi, (high_token + PAGE) / PAGE), w.lo) : w.lo;
-    const int my_lo = min_of(my_hi, max_of(w.lo, a.window > 0 && low_token >= a.window ? (low_token - a.window + 1) / PAGE : 0));
+    const int my_lo = min_of(my_hi, max_of(w.lo, a.window > 0 && lowest >= a.window ? (lowest - a.window + 1) / PAGE : 0));
     uint32_t now = 0, next = 0;                            // scales of the page that is read and of the one in my registers
     int p = w.lo;
     ldsptr here = ring + lane * 16, there = ring + 2 * PAGE_BYTES;           // the page that is read (for this lane), and the next one's place
@@ -745,12 +812,19 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
         }
         if (p * PAGE + PAGE - 1 > low_token || (a.window > 0 && p * PAGE <= high_token - a.window)) {
             const int last = last_key - p * PAGE - 16 * h, from = first_key - p * PAGE - 16 * h;
+            if (tree) {
+                const uint64_t seen = seen_of_page(bits, p * PAGE - w.s.start) >> (16 * h);
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
+                for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) z[u][i] = 32 * u + i > last || 32 * u + i < from ? -INFINITY : z[u][i] * unit[u];
-                unit[u] = 1.f;
+                    for (int i = 0; i < 16; ++i) z[u][i] = !(static_cast<uint32_t>(seen >> (32 * u)) >> i & 1) || 32 * u + i < from ? -INFINITY : z[u][i] * unit[u];
+            } else {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[u][i] = 32 * u + i > last || 32 * u + i < from ? -INFINITY : z[u][i] * unit[u];
             }
+            unit[0] = unit[1] = 1.f;
         }
         auto scale_sums = [&](float f) {
 #pragma unroll
@@ -885,37 +959,55 @@ __device__ __forceinline__ void attend_many(const work_item& w, const int32_t* _
         }
 }
 
-__global__ __launch_bounds__(NT, 2) void attend_many_kernel(const epara_cache_attn_args* __restrict__ args, const epara_sequence* __restrict__ seqs,
-                                                           const int32_t* __restrict__ pages, const int32_t* __restrict__ first, int n_seqs, int part_pages,
-                                                           uint32_t* counters, char* slots)
+template <bool TREE>
+__global__ __launch_bounds__(NT, 2) void attend_many_kernel(const epara_cache_attn_args* __restrict__ args, const epara_tree_args* __restrict__ trees,
+                                                           const epara_sequence* __restrict__ seqs, const int32_t* __restrict__ pages, const int32_t* __restrict__ first,
+                                                           int n_seqs, int part_pages, uint32_t* counters, char* slots)
 {
     __shared__ __attribute__((aligned(1024))) char ring[2 * 4 * PAGE * 128];        // two pages in f16: one is read, one on its way
     const int item = blockIdx.x;
-    const work_item w = find_work<MANY_TILE>(args, seqs, first, n_seqs, part_pages, item, threadIdx.x & 63);
+    const work_item w = find_work<MANY_TILE, TREE>(args, trees, seqs, first, n_seqs, part_pages, item, threadIdx.x & 63);
     if (w.part > 0 && w.part >= w.parts) return;
-    if (w.a.head_dim == 128) attend_many<128>(w, pages, counters, slots, (ldsptr)ring, item);
-    else                     attend_many<64>(w, pages, counters, slots, (ldsptr)ring, item);
+    if (w.a.head_dim == 128) attend_many<128, TREE>(w, pages, counters, slots, (ldsptr)ring, item);
+    else                     attend_many<64, TREE>(w, pages, counters, slots, (ldsptr)ring, item);
 }
 
-}  // namespace
-
-extern "C" int32_t epara_cache_attention(const epara_cache_attn_launch* launch, void* stream)
+template <bool TREE>
+int32_t launch_attention(const epara_cache_attn_launch& l, const epara_tree_args* d_trees, const bool cut[2], void* stream)
 {
-    if (!launch) return EPARA_ERR_NULL;
-    const epara_cache_attn_launch& l = *launch;
-    bool cut[2];
-    if (const int32_t rc = epara_check_attn_call(l, cut)) return rc;
     if (l.plan.n_items[0] + l.plan.n_items[1] == 0 || l.table.n_seqs == 0) return EPARA_OK;
-    if (!l.d_args || !l.d_first) return EPARA_ERR_NULL;
+    if (!l.d_args || !l.d_first || (TREE && !d_trees)) return EPARA_ERR_NULL;
     uint32_t* counters = static_cast<uint32_t*>(l.d_workspace);
     char* slots = static_cast<char*>(l.d_workspace) + epara_attn_counter_bytes(l.plan.n_items);
     char* many_slots = slots + (cut[0] ? static_cast<size_t>(l.plan.n_items[0]) * FEW_TILE * SLOT_FLOATS * 4 : 0);
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (l.plan.n_items[1] > 0)
-        hipLaunchKernelGGL(attend_many_kernel, dim3(static_cast<unsigned>(l.plan.n_items[1])), dim3(NT), 0, s, l.d_args, l.table.d_seqs, l.table.d_pages,
+        hipLaunchKernelGGL(attend_many_kernel<TREE>, dim3(static_cast<unsigned>(l.plan.n_items[1])), dim3(NT), 0, s, l.d_args, d_trees, l.table.d_seqs, l.table.d_pages,
                            l.d_first + l.table.n_seqs + 1, l.table.n_seqs, l.plan.part_pages[1], counters + l.plan.n_items[0], many_slots);
     if (l.plan.n_items[0] > 0)
-        hipLaunchKernelGGL(attend_few_kernel, dim3(static_cast<unsigned>(l.plan.n_items[0])), dim3(NT), 0, s, l.d_args, l.table.d_seqs, l.table.d_pages, l.d_first,
+        hipLaunchKernelGGL(attend_few_kernel<TREE>, dim3(static_cast<unsigned>(l.plan.n_items[0])), dim3(NT), 0, s, l.d_args, d_trees, l.table.d_seqs, l.table.d_pages, l.d_first,
                            l.table.n_seqs, l.plan.part_pages[0], counters, slots);
     return hipGetLastError() == hipSuccess ? EPARA_OK : EPARA_ERR_HIP;
 }
+
+}  // namespace
+
+extern "C" {
+
+int32_t epara_cache_attention(const epara_cache_attn_launch* launch, void* stream)
+{
+    if (!launch) return EPARA_ERR_NULL;
+    bool cut[2];
+    if (const int32_t rc = epara_check_attn_call(*launch, cut)) return rc;
+    return launch_attention<false>(*launch, nullptr, cut, stream);
+}
+
+int32_t epara_tree_attention(const epara_cache_attn_launch* launch, const epara_tree_args* h_trees, const epara_tree_args* d_trees, void* stream)
+{
+    if (!launch || (launch->G > 0 && !h_trees)) return EPARA_ERR_NULL;
+    bool cut[2];
+    if (const int32_t rc = epara_check_attn_call(*launch, cut, h_trees)) return rc;
+    return launch_attention<true>(*launch, d_trees, cut, stream);
+}
+
+}  // extern "C"

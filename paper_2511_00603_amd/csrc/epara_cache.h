@@ -59,14 +59,19 @@ constexpr int SLOT_FLOATS = 128 + 4;                       // per row of a part:
 EPARA_BOTH bool has_few_rows(const epara_cache_attn_args& a, const epara_sequence& s) { return static_cast<int64_t>(s.rows) * (a.heads / a.kv_heads) <= FEW_MAX_ROWS; }
 
 struct page_range { int lo, hi; };
-// Pages that hold a key which the tokens first .. last of a sequence (by row) see; lo = hi = 0: none.
-EPARA_BOTH page_range pages_of_tokens(const epara_sequence& s, int window, int first, int last)
+// Pages that hold a key which the new rows first .. last of a sequence see; lo = hi = 0: none.  A row of a tree lies behind all rows that it follows, so it sees no key
+// behind its own, but its position may be as low as the tree's first row's.
+EPARA_BOTH page_range pages_of_rows(const epara_sequence& s, int window, bool tree, int first, int last)
 {
-    const int from = s.start + first, to = s.start + last;
+    const int from = s.start + (tree ? 0 : first), to = s.start + last;
     if (to < 0) return {0, 0};
     const int lo = window > 0 && from >= window ? from - window + 1 : 0;
     return {lo / PAGE, to / PAGE + 1};
 }
+
+// ---- trees of drafted tokens: a sequence of up to EPARA_TREE_MAX_ROWS new rows is one where its service has bits of them
+constexpr int TREE_ROWS = EPARA_TREE_MAX_ROWS, TREE_WORDS = TREE_ROWS / 64;
+EPARA_BOTH bool is_tree(const epara_tree_args* trees, const epara_sequence& s) { return trees && s.rows <= TREE_ROWS && trees[s.service].visible; }
 
 }  // namespace epara_cache
 

@@ -2,6 +2,7 @@
 // Nothing here touches the GPU; no exception leaves an entry point.
 #include "epara.h"
 #include "epara_cache.h"
+#include "epara_cache_checks.h"
 #include "epara_cache_host.h"
 
 #include <algorithm>
@@ -9,49 +10,12 @@
 #include <cmath>
 #include <functional>
 #include <new>
+#include <utility>
 #include <vector>
 
 using namespace epara_cache;
 
 namespace {
-
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-inline bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
-
-bool bad_heads(int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t n_pages)
-{
-    return heads < 1 || kv_heads < 1 || heads % kv_heads != 0 || heads / kv_heads > EPARA_CACHE_MAX_GROUP || heads > 65536 || (head_dim != 64 && head_dim != 128) || n_pages < 0;
-}
-
-// The sequences of a call against the services' rows and the page table.
-template <class Args>
-int32_t check_sequences(const Args* args, int32_t G, const epara_sequence_table* t)
-{
-    if (!t) return EPARA_ERR_NULL;
-    if (t->n_seqs < 0 || t->n_table < 0) return EPARA_ERR_SHAPE;
-    if (t->n_seqs > 0 && (!t->h_seqs || !t->d_seqs)) return EPARA_ERR_NULL;
-    if (t->n_table > 0 && (!t->h_pages || !t->d_pages)) return EPARA_ERR_NULL;
-    int32_t service = 0;
-    for (int32_t i = 0; i < t->n_seqs; ++i) {
-        const epara_sequence& s = t->h_seqs[i];
-        if (s.service < service || s.service >= G) return EPARA_ERR_SHAPE;
-        service = s.service;
-        if (s.rows < 0 || s.first_row < 0 || static_cast<int64_t>(s.first_row) + s.rows > args[service].rows) return EPARA_ERR_SHAPE;
-        if (s.first_page < 0 || s.n_pages < 0 || static_cast<int64_t>(s.first_page) + s.n_pages > t->n_table) return EPARA_ERR_SHAPE;
-        if (s.start < -EPARA_CACHE_MAX_TOKENS || static_cast<int64_t>(s.start) + s.rows > std::min<int64_t>(EPARA_CACHE_MAX_TOKENS, static_cast<int64_t>(s.n_pages) * PAGE)) return EPARA_ERR_SHAPE;
-    }
-    return EPARA_OK;
-}
-
-// The pages [lo, hi) of a sequence lie inside its service's cache.
-bool pages_inside(const epara_sequence_table* t, const epara_sequence& s, int lo, int hi, int32_t n_pages)
-{
-    for (int p = lo; p < hi; ++p) {
-        const int32_t id = t->h_pages[s.first_page + p];
-        if (id < 0 || id >= n_pages) return false;
-    }
-    return true;
-}
 
 int32_t check_append(const epara_append_args* args, int32_t G, const epara_sequence_table* t)
 {
@@ -78,32 +42,6 @@ int32_t check_append(const epara_append_args* args, int32_t G, const epara_seque
         if (!pages_inside(t, s, std::max(s.start, 0) / PAGE, (end - 1) / PAGE + 1, a.n_pages)) return EPARA_ERR_SHAPE;
     }
     return EPARA_OK;
-}
-
-// No row is written for two sequences of a service; writes(args): whether that service's rows are.  Sequences in the order of their rows, as a rule, need no list.
-template <class Args, class Writes>
-int32_t check_rows_once(const Args* args, const epara_sequence_table* t, Writes writes)
-{
-    bool ordered = true;
-    int32_t service = -1, end = 0;
-    for (int32_t i = 0; i < t->n_seqs && ordered; ++i) {
-        const epara_sequence& s = t->h_seqs[i];
-        if (s.rows == 0 || !writes(args[s.service])) continue;
-        ordered = s.service != service || s.first_row >= end;
-        service = s.service;
-        end = s.first_row + s.rows;
-    }
-    if (ordered) return EPARA_OK;
-    try {
-        std::vector<epara_sequence> seqs;
-        for (int32_t i = 0; i < t->n_seqs; ++i)
-            if (t->h_seqs[i].rows > 0 && writes(args[t->h_seqs[i].service])) seqs.push_back(t->h_seqs[i]);
-        std::sort(seqs.begin(), seqs.end(), [](const epara_sequence& a, const epara_sequence& b) { return a.service != b.service ? a.service < b.service : a.first_row < b.first_row; });
-        const auto meet = [](const epara_sequence& a, const epara_sequence& b) { return a.service == b.service && b.first_row < a.first_row + a.rows; };
-        return std::adjacent_find(seqs.begin(), seqs.end(), meet) == seqs.end() ? EPARA_OK : EPARA_ERR_SHAPE;
-    } catch (const std::bad_alloc&) {
-        return EPARA_ERR_CAPACITY;
-    }
 }
 
 // No page of a cache is written for two sequences (or twice for one).
@@ -136,7 +74,8 @@ int32_t count_append(const epara_append_args* args, const epara_sequence_table* 
     return EPARA_OK;
 }
 
-int32_t check_attn(const epara_cache_attn_args* args, int32_t G, const epara_sequence_table* t)
+// trees: of epara_tree_attention, else NULL.
+int32_t check_attn(const epara_cache_attn_args* args, int32_t G, const epara_sequence_table* t, const epara_tree_args* trees)
 {
     if (G < 0) return EPARA_ERR_SHAPE;
     if (G > 0 && !args) return EPARA_ERR_NULL;
@@ -148,6 +87,8 @@ int32_t check_attn(const epara_cache_attn_args* args, int32_t G, const epara_seq
         if (a.rows > 0 && (!a.Q || !a.O || !a.codes || !a.scales)) return EPARA_ERR_NULL;
         if (a.rows > 0 && a.Q == a.O) return EPARA_ERR_SHAPE;
         if (misaligned(a.Q, 16) || misaligned(a.O, 16) || misaligned(a.codes, 16) || misaligned(a.scales, 4)) return EPARA_ERR_ALIGN;
+        if (trees && trees[g].visible && trees[g].rows != a.rows) return EPARA_ERR_SHAPE;
+        if (trees && misaligned(trees[g].visible, 16)) return EPARA_ERR_ALIGN;
     }
     if (const int32_t rc = check_sequences(args, G, t)) return rc;
     for (int32_t i = 0; i < t->n_seqs; ++i) {
@@ -155,7 +96,9 @@ int32_t check_attn(const epara_cache_attn_args* args, int32_t G, const epara_seq
         const epara_cache_attn_args& a = args[s.service];
         if (s.rows == 0) continue;
         if (static_cast<int64_t>(s.rows) * (a.heads / a.kv_heads) > INT32_MAX / 2) return EPARA_ERR_CAPACITY;
-        const page_range r = pages_of_tokens(s, a.window, std::min(std::max(-s.start, 0), s.rows - 1), s.rows - 1);
+        const bool tree = is_tree(trees, s);
+        if (tree && (s.start < 0 || (a.window > 0 && a.window < s.rows))) return EPARA_ERR_SHAPE;
+        const page_range r = pages_of_rows(s, a.window, tree, std::min(std::max(-s.start, 0), s.rows - 1), s.rows - 1);
         if (!pages_inside(t, s, r.lo, r.hi, a.n_pages)) return EPARA_ERR_SHAPE;
     }
     return EPARA_OK;
@@ -168,14 +111,14 @@ seq_tiles tiles_of(const epara_cache_attn_args& a, const epara_sequence& s)
     return {few, static_cast<int>(ceil_div(static_cast<int64_t>(s.rows) * (a.heads / a.kv_heads), few ? FEW_TILE : MANY_TILE))};
 }
 
-page_range pages_of_tile(const epara_cache_attn_args& a, const epara_sequence& s, int few, int tile)
+page_range pages_of_tile(const epara_cache_attn_args& a, const epara_sequence& s, bool tree, int few, int tile)
 {
     const int group = a.heads / a.kv_heads, size = few ? FEW_TILE : MANY_TILE, rows = s.rows * group;
-    return pages_of_tokens(s, a.window, tile * size / group, (std::min(rows, tile * size + size) - 1) / group);
+    return pages_of_rows(s, a.window, tree, tile * size / group, (std::min(rows, tile * size + size) - 1) / group);
 }
 
 // Running sums of workgroups of both kinds of sequences, with parts of part_pages pages.
-int32_t count_attn(const epara_cache_attn_args* args, const epara_sequence_table* t, const int32_t part_pages[2], int32_t* first, const int32_t* expected,
+int32_t count_attn(const epara_cache_attn_args* args, const epara_sequence_table* t, const epara_tree_args* trees, const int32_t part_pages[2], int32_t* first, const int32_t* expected,
                    int32_t n_items[2], bool cut[2])
 {
     int64_t items[2] = {0, 0};
@@ -193,7 +136,7 @@ int32_t count_attn(const epara_cache_attn_args* args, const epara_sequence_table
         const int k = w.few ? 0 : 1;
         int64_t parts = 1;
         for (int tile = 0; tile < w.tiles; ++tile) {
-            const page_range r = pages_of_tile(a, s, w.few, tile);
+            const page_range r = pages_of_tile(a, s, is_tree(trees, s), w.few, tile);
             parts = std::max(parts, ceil_div(r.hi - r.lo, part_pages[k]));
         }
         if (parts > MAX_PARTS) return EPARA_ERR_SHAPE;
@@ -213,6 +156,32 @@ int64_t attn_workspace(const int32_t n_items[2], const bool cut[2])
            (cut[1] ? static_cast<int64_t>(n_items[1]) * MANY_TILE * SLOT_FLOATS * 4 : 0);
 }
 
+int32_t plan_attn(const epara_cache_attn_args* h_args, const epara_tree_args* trees, int32_t G, const epara_sequence_table* table, int32_t n_compute_units,
+                  int32_t* first, epara_cache_attn_plan* plan)
+{
+    if (const int32_t rc = check_attn(h_args, G, table, trees)) return rc;
+    if (!first || !plan) return EPARA_ERR_NULL;
+    if (n_compute_units < 1 || n_compute_units > 65536) return EPARA_ERR_SHAPE;
+    int64_t work[2] = {0, 0}, longest[2] = {0, 0};
+    for (int32_t i = 0; i < table->n_seqs; ++i) {
+        const epara_sequence& s = table->h_seqs[i];
+        const epara_cache_attn_args& a = h_args[s.service];
+        if (s.rows == 0) continue;
+        const seq_tiles w = tiles_of(a, s);
+        const int k = w.few ? 0 : 1;
+        for (int tile = 0; tile < w.tiles; ++tile) {
+            const page_range r = pages_of_tile(a, s, is_tree(trees, s), w.few, tile);
+            work[k] += static_cast<int64_t>(r.hi - r.lo) * a.kv_heads;
+            longest[k] = std::max<int64_t>(longest[k], r.hi - r.lo);
+        }
+    }
+    epara_attn_part_pages(work, longest, n_compute_units, plan->part_pages);
+    bool cut[2];
+    if (const int32_t rc = count_attn(h_args, table, trees, plan->part_pages, first, nullptr, plan->n_items, cut)) return rc;
+    plan->workspace_bytes = attn_workspace(plan->n_items, cut);
+    return EPARA_OK;
+}
+
 }  // namespace
 
 int32_t epara_check_append_call(const epara_append_args* h_args, int32_t G, const epara_sequence_table* table, const int32_t* h_first)
@@ -225,15 +194,15 @@ int32_t epara_check_append_call(const epara_append_args* h_args, int32_t G, cons
     return check_written_once(h_args, table);
 }
 
-int32_t epara_check_attn_call(const epara_cache_attn_launch& l, bool cut[2])
+int32_t epara_check_attn_call(const epara_cache_attn_launch& l, bool cut[2], const epara_tree_args* trees)
 {
-    if (const int32_t rc = check_attn(l.h_args, l.G, &l.table)) return rc;
+    if (const int32_t rc = check_attn(l.h_args, l.G, &l.table, trees)) return rc;
     cut[0] = cut[1] = false;
     if (l.table.n_seqs == 0) return EPARA_OK;
     if (!l.h_first) return EPARA_ERR_NULL;
     if (l.plan.part_pages[0] < 1 || l.plan.part_pages[1] < 1) return EPARA_ERR_SHAPE;
     int32_t n[2];
-    if (const int32_t rc = count_attn(l.h_args, &l.table, l.plan.part_pages, nullptr, l.h_first, n, cut)) return rc;
+    if (const int32_t rc = count_attn(l.h_args, &l.table, trees, l.plan.part_pages, nullptr, l.h_first, n, cut)) return rc;
     if (n[0] != l.plan.n_items[0] || n[1] != l.plan.n_items[1]) return EPARA_ERR_SHAPE;
     if (const int32_t rc = check_rows_once(l.h_args, &l.table, [](const epara_cache_attn_args&) { return true; })) return rc;
     const int64_t bytes = attn_workspace(n, cut);
@@ -318,27 +287,14 @@ int32_t epara_plan_cache_append(const epara_append_args* h_args, int32_t G, cons
 int32_t epara_plan_cache_attention(const epara_cache_attn_args* h_args, int32_t G, const epara_sequence_table* table, int32_t n_compute_units,
                                    int32_t* first, epara_cache_attn_plan* plan)
 {
-    if (const int32_t rc = check_attn(h_args, G, table)) return rc;
-    if (!first || !plan) return EPARA_ERR_NULL;
-    if (n_compute_units < 1 || n_compute_units > 65536) return EPARA_ERR_SHAPE;
-    int64_t work[2] = {0, 0}, longest[2] = {0, 0};
-    for (int32_t i = 0; i < table->n_seqs; ++i) {
-        const epara_sequence& s = table->h_seqs[i];
-        const epara_cache_attn_args& a = h_args[s.service];
-        if (s.rows == 0) continue;
-        const seq_tiles w = tiles_of(a, s);
-        const int k = w.few ? 0 : 1;
-        for (int tile = 0; tile < w.tiles; ++tile) {
-            const page_range r = pages_of_tile(a, s, w.few, tile);
-            work[k] += static_cast<int64_t>(r.hi - r.lo) * a.kv_heads;
-            longest[k] = std::max<int64_t>(longest[k], r.hi - r.lo);
-        }
-    }
-    epara_attn_part_pages(work, longest, n_compute_units, plan->part_pages);
-    bool cut[2];
-    if (const int32_t rc = count_attn(h_args, table, plan->part_pages, first, nullptr, plan->n_items, cut)) return rc;
-    plan->workspace_bytes = attn_workspace(plan->n_items, cut);
-    return EPARA_OK;
+    return plan_attn(h_args, nullptr, G, table, n_compute_units, first, plan);
+}
+
+int32_t epara_plan_tree_attention(const epara_cache_attn_args* h_args, const epara_tree_args* h_trees, int32_t G, const epara_sequence_table* table, int32_t n_compute_units,
+                                  int32_t* first, epara_cache_attn_plan* plan)
+{
+    if (G > 0 && !h_trees) return EPARA_ERR_NULL;
+    return plan_attn(h_args, h_trees, G, table, n_compute_units, first, plan);
 }
 
 int32_t epara_page_pool_init(epara_page_pool* pool, int32_t* refs, int32_t* free_pages, int32_t n_pages)

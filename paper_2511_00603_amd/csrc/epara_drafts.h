@@ -1,0 +1,42 @@
+// What the host half of decoding by drafts and its kernels have to agree on: how verification is cut into work, and its workspace.
+#ifndef EPARA_DRAFTS_H
+#define EPARA_DRAFTS_H
+
+#include <stdint.h>
+
+#include "epara.h"
+#include "epara_cache.h"
+#include "epara_plan.h"
+
+namespace epara_drafts {
+
+using epara_cache::TREE_ROWS;
+
+// ---- verification.  A row of logits is taken in pieces of 16 bytes from the 16-byte boundary at or before its first element; a workgroup takes 256 * `pieces` of them.  A row
+// of which nothing is known about alignment has up to one piece more than its length says.
+EPARA_BOTH int element_bytes(int dtype) { return dtype == EPARA_F32 ? 4 : 2; }
+EPARA_BOTH int pieces_of_row(int vocab, int dtype)
+{
+    const int per = 16 / element_bytes(dtype);
+    return (vocab - 1 + per - 1) / per + 1;                // ceil((vocab + per - 1) / per)
+}
+EPARA_BOTH int chunks_of_row(int vocab, int dtype, int pieces) { return (pieces_of_row(vocab, dtype) + 256 * pieces - 1) / (256 * pieces); }
+
+// The first kernel has a workgroup for each chunk of each row's logits, and of its draft logits behind those.
+struct row_sum { float top; int32_t at; double sum; };     // of a chunk: the largest logit, where it is (greedy sequences only), sum of exp((x - top) / T)
+EPARA_BOTH int64_t rows_items(const epara_verify_args& a, const epara_sequence& s, int chunks) { return static_cast<int64_t>(s.rows) * chunks * (a.draft_logits ? 2 : 1); }
+
+// The second kernel has a workgroup for each chunk of one row of each sequence, and so has the third.
+struct chunk_sum { double p, q, rest; };                   // of the weights of p, of q, and of max(p - q, 0)
+struct drawn_row { int32_t row; float top_p, top_q; int32_t reserved; };         // behind which the third kernel draws a token; -1: it need not
+
+// Workspace: a counter per sequence, drawn_row of each, then the first kernel's sums, then chunk_sum of each workgroup of the second.
+EPARA_BOTH int64_t counter_bytes(int n_seqs) { return (static_cast<int64_t>(n_seqs) * 4 + 255) & ~static_cast<int64_t>(255); }
+
+}  // namespace epara_drafts
+
+EPARA_HIDDEN int32_t epara_check_trees_call(const epara_tree_args* h_args, int32_t G, const epara_sequence_table* table);
+EPARA_HIDDEN int32_t epara_check_verify_call(const epara_verify_launch& launch);
+EPARA_HIDDEN int32_t epara_check_keep_call(const epara_keep_args* h_caches, int32_t n_caches, const epara_sequence_table* table, int32_t* n_items);
+
+#endif

@@ -439,8 +439,8 @@ class CacheAttnPlan:
             self.args[i] = (_want(g["Q"], bf, (rows, H * D), "Q", strided=True), _want(g["O"], bf, (rows, H * D), "O", strided=True),
                             c.codes.data_ptr(), c.scales.data_ptr(), rows, H, c.kv_heads, D, c.n_pages, _row_stride(g["Q"]), _row_stride(g["O"]),
                             int(g.get("window") or 0), D ** -0.5 if g.get("scale") is None else float(g["scale"]), float(g.get("softcap") or 0.0), (0, 0))
-        self.first, self.plan = B.epara_plan_cache_attention(self.args, table.c, n_compute_units(device))
-        self.d_args, self.d_first = _upload_all([self.args, self.first], device)
+        self.first, self.plan = self._cut(groups, n_compute_units(device))
+        self._upload(device)
         self.d_workspace, at = None, 0
         if self.plan.workspace_bytes:
             self.d_workspace = torch.empty(self.plan.workspace_bytes, dtype=torch.uint8, device=device)
@@ -451,10 +451,41 @@ class CacheAttnPlan:
                                    self.plan.workspace_bytes, table.c, self.plan, len(self.args), 0)
         torch.cuda.synchronize(device)
         self._keep = groups
-        self._call = B.Call("epara_cache_attention", ctypes.addressof(self.c))
+        self._call = self._bind()
+
+    def _cut(self, groups, units):
+        return B.epara_plan_cache_attention(self.args, self.table.c, units)
+
+    def _upload(self, device):
+        self.d_args, self.d_first = _upload_all([self.args, self.first], device)
+
+    def _bind(self):
+        return B.Call("epara_cache_attention", ctypes.addressof(self.c))
 
 
 def cache_attention(plan, stream=None):
+    plan._call(_stream_of_call() if stream is None else stream)
+
+
+class TreeAttnPlan(CacheAttnPlan):
+    """Arguments of one epara_tree_attention call: groups as of CacheAttnPlan, with visible (int64 [rows, 4], as epara_draft_trees writes it) where a service's sequences
+    are trees."""
+
+    def _cut(self, groups, units):
+        self.trees = np.zeros(len(groups), dtype=B.TREE_ARGS)
+        for i, g in enumerate(groups):
+            rows = int(g["Q"].shape[0])
+            self.trees[i] = (0, _want(g.get("visible"), torch.int64, (rows, B.EPARA_TREE_MAX_ROWS // 64), "visible", True), 0, rows, 0)
+        return B.epara_plan_tree_attention(self.args, self.trees, self.table.c, units)
+
+    def _upload(self, device):
+        self.d_args, self.d_first, self.d_trees = _upload_all([self.args, self.first, self.trees], device)
+
+    def _bind(self):
+        return B.Call("epara_tree_attention", ctypes.addressof(self.c), self.trees.ctypes.data, self.d_trees.data_ptr())
+
+
+def tree_attention(plan, stream=None):
     plan._call(_stream_of_call() if stream is None else stream)
 
 
@@ -483,6 +514,102 @@ class PageCopyPlan:
 
 
 def copy_pages(plan, stream=None):
+    plan._call(_stream_of_call() if stream is None else stream)
+
+
+# ---- decoding by drafts ---------------------------------------------------------------------------------
+
+class DraftTreePlan:
+    """Arguments of one epara_draft_trees call.  groups: per service of the table a dict with parents (int32 [rows]) and optionally visible (int64 [rows, 4], the
+    bits of 256 rows) and positions (int32 [rows, 3]), both written; made here where they are not given (self.groups)."""
+
+    def __init__(self, table, groups, device):
+        _require_gpu()
+        if len(groups) != table.G:
+            raise ValueError("%d services in the table, %d groups" % (table.G, len(groups)))
+        self.table, self.groups, self.args = table, [], np.zeros(len(groups), dtype=B.TREE_ARGS)
+        for i, g in enumerate(groups):
+            rows, out = int(g["parents"].shape[0]), {"parents": g["parents"]}
+            for name, shape, dtype in (("visible", (rows, B.EPARA_TREE_MAX_ROWS // 64), torch.int64), ("positions", (rows, 3), torch.int32)):
+                out[name] = torch.zeros(shape, dtype=dtype, device=device) if g.get(name) is None else g[name]
+            self.groups.append(out)
+            self.args[i] = (_want(out["parents"], torch.int32, (rows,), "parents"), _want(out["visible"], torch.int64, (rows, B.EPARA_TREE_MAX_ROWS // 64), "visible"),
+                            _want(out["positions"], torch.int32, (rows, 3), "positions"), rows, 0)
+        self.d_args = _upload(self.args, device)
+        self._call = B.Call("epara_draft_trees", self.args.ctypes.data, self.d_args.data_ptr(), len(groups), ctypes.addressof(table.c))
+
+
+def draft_trees(plan, stream=None):
+    plan._call(_stream_of_call() if stream is None else stream)
+
+
+class VerifyPlan:
+    """Arguments of one epara_verify_drafts call.  groups: per service of the table a dict with logits [rows, vocab] (bf16 or float32, the same for all services), tokens
+    (int32 [rows]), uniforms (float32 [rows]) and optionally parents (int32 [rows]; left out: chains), draft_logits [rows, vocab], and the outputs path (int32 [rows]) and
+    probs (float32 [rows]), made here where they are not given (self.groups).  temperatures: float32 [sequences of the table], or None (greedy).  Per sequence of
+    the table, written: self.kept and self.next (int32)."""
+
+    def __init__(self, table, groups, device, temperatures=None, kept=None, next=None):
+        _require_gpu()
+        if len(groups) != table.G:
+            raise ValueError("%d services in the table, %d groups" % (table.G, len(groups)))
+        kinds = {g["logits"].dtype for g in groups}
+        if len(kinds) > 1 or not kinds <= {torch.bfloat16, torch.float32}:
+            raise ValueError("logits: bfloat16 or float32 for all services of a call")
+        kind = kinds.pop() if kinds else torch.bfloat16
+        self.table, self.groups, self.args = table, [], np.zeros(len(groups), dtype=B.VERIFY_ARGS)
+        self.dtype = B.EPARA_F32 if kind == torch.float32 else B.EPARA_BF16
+        i32, f32, n = torch.int32, torch.float32, len(table.seqs)
+        for i, g in enumerate(groups):
+            rows, vocab = (int(v) for v in g["logits"].shape)
+            out = dict(g)
+            for name, dtype in (("path", i32), ("probs", f32)):
+                if g.get(name) is None:
+                    out[name] = torch.zeros(rows, dtype=dtype, device=device)
+            self.groups.append(out)
+            draft = g.get("draft_logits")
+            self.args[i] = (_want(g["logits"], kind, (rows, vocab), "logits", strided=True), _want(draft, kind, (rows, vocab), "draft_logits", True, True),
+                            _want(g["tokens"], i32, (rows,), "tokens"), _want(g.get("parents"), i32, (rows,), "parents", True), _want(g["uniforms"], f32, (rows,), "uniforms"),
+                            _want(out["path"], i32, (rows,), "path"), _want(out["probs"], f32, (rows,), "probs"), rows, vocab, _row_stride(g["logits"]),
+                            0 if draft is None else _row_stride(draft))
+        self.kept, self.next = (torch.zeros(n, dtype=i32, device=device) if t is None else t for t in (kept, next))
+        self.temperatures = temperatures
+        at = [_want(temperatures, f32, (n,), "temperatures", True), _want(self.kept, i32, (n,), "kept"), _want(self.next, i32, (n,), "next")]
+        self.first, self.plan = B.epara_plan_verify_drafts(self.args, table.c, self.dtype, n_compute_units(device))
+        self.d_args, self.d_first = _upload_all([self.args, self.first], device)
+        self.d_workspace = torch.empty(max(self.plan.workspace_bytes, 256), dtype=torch.uint8, device=device)
+        B.epara_workspace_init(self.d_workspace.data_ptr(), -(-max(4 * n, 1) // 256) * 256, current_stream_handle())
+        self.c = B.VerifyLaunch(self.args.ctypes.data, self.d_args.data_ptr(), self.first.ctypes.data, self.d_first.data_ptr(), *(p or None for p in at),
+                                self.d_workspace.data_ptr(), self.plan.workspace_bytes, table.c, self.plan, len(self.args), self.dtype)
+        torch.cuda.synchronize(device)
+        self._call = B.Call("epara_verify_drafts", ctypes.addressof(self.c))
+
+
+def verify_drafts(plan, stream=None):
+    plan._call(_stream_of_call() if stream is None else stream)
+
+
+class CacheKeepPlan:
+    """Arguments of one epara_cache_keep call.  groups: per cache (a layer of a service) a dict with service, cache (PagedCache) and path (int32 [rows of the service]);
+    kept: int32 [sequences of the table], both as epara_verify_drafts writes them."""
+
+    def __init__(self, table, groups, device, kept):
+        _require_gpu()
+        self.table, self.args, items = table, np.zeros(len(groups), dtype=B.KEEP_ARGS), 0
+        service = np.ascontiguousarray(table.seqs["service"])
+        for i, g in enumerate(groups):
+            c, rows = g["cache"], int(g["path"].shape[0])
+            first, end = (int(v) for v in np.searchsorted(service, [g["service"], g["service"] + 1]))
+            self.args[i] = (c.codes.data_ptr(), c.scales.data_ptr(), _want(g["path"], torch.int32, (rows,), "path"), int(g["service"]), first, rows, c.n_pages,
+                            c.kv_heads, c.head_dim, items, 0)
+            items += (end - first) * c.kv_heads
+        self.d_args = _upload(self.args, device)
+        self._keep = groups, kept
+        self._call = B.Call("epara_cache_keep", self.args.ctypes.data, self.d_args.data_ptr(), len(groups), ctypes.addressof(table.c),
+                            _want(kept, torch.int32, (len(table.seqs),), "kept") or None)
+
+
+def cache_keep(plan, stream=None):
     plan._call(_stream_of_call() if stream is None else stream)
 
 
