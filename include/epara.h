@@ -1064,19 +1064,19 @@ typedef struct {
     int32_t stride, draft_stride; /* >= vocab */
 } epara_verify_args;
 
-/* How a call is cut into work: made by epara_plan_verify_drafts.  first[0 .. n_seqs] and first[n_seqs + 1 .. 2 n_seqs + 1] are running sums of the workgroups of the
- * sequences that read the rows' logits, and that draw the next token. */
+/* How a call is cut into work: made by epara_plan_verify_drafts.  first[0 .. n_seqs] are running sums of the workgroups of the sequences that read the rows' logits. */
 typedef struct {
-    int32_t n_items[2];
-    int32_t pieces;               /* a workgroup takes 256 * pieces pieces of 16 bytes of a row: 1, 2, 4 or 8 */
-    int32_t reserved;
+    int32_t n_items;              /* of these workgroups */
+    int32_t pieces;               /* each takes 256 * pieces pieces of 16 bytes of a row: 1, 2, 4 or 8 */
+    int32_t draw_chunks;          /* workgroups that draw the next token of a sequence */
+    int32_t draw_pieces;          /* each takes 256 * draw_pieces pieces of the last row's: 1, 2 or 4 */
     int64_t workspace_bytes;
 } epara_verify_plan;
 
 typedef struct {
     const epara_verify_args* h_args;
     const epara_verify_args* d_args;
-    const int32_t* h_first;       /* int32[2 * (n_seqs + 1)] */
+    const int32_t* h_first;       /* int32[n_seqs + 1] */
     const int32_t* d_first;
     const float* d_temperatures;  /* device, fp32 [n_seqs]; NULL: all 0 */
     int32_t*     d_kept;          /* device, int32 [n_seqs], out: rows that stay, the first among them; 0 for a sequence without rows */

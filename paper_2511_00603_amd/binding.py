@@ -122,7 +122,7 @@ class CacheAttnLaunch(ctypes.Structure):
 
 class VerifyPlan(ctypes.Structure):
     """struct epara_verify_plan."""
-    _fields_ = [("n_items", ctypes.c_int32 * 2), ("pieces", ctypes.c_int32), ("reserved", ctypes.c_int32), ("workspace_bytes", ctypes.c_int64)]
+    _fields_ = [("n_items", ctypes.c_int32), ("pieces", ctypes.c_int32), ("draw_chunks", ctypes.c_int32), ("draw_pieces", ctypes.c_int32), ("workspace_bytes", ctypes.c_int64)]
 
 
 class VerifyLaunch(ctypes.Structure):
@@ -453,9 +453,9 @@ def epara_tree_attention(launch, h_trees, d_trees, stream=0):
 
 
 def epara_plan_verify_drafts(h_args, table, dtype, n_compute_units):
-    """h_args: VERIFY_ARGS[G] -> (running sums int32[2 (n_seqs + 1)], VerifyPlan)."""
+    """h_args: VERIFY_ARGS[G] -> (running sums int32[n_seqs + 1], VerifyPlan)."""
     h_args = np.ascontiguousarray(h_args, dtype=VERIFY_ARGS)
-    first, plan = np.zeros(2 * (table.n_seqs + 1), dtype=np.int32), VerifyPlan()
+    first, plan = np.zeros(table.n_seqs + 1, dtype=np.int32), VerifyPlan()
     _check(lib().epara_plan_verify_drafts(_ptr(h_args) if len(h_args) else None, len(h_args), ctypes.addressof(table), int(dtype), int(n_compute_units),
                                           _ptr(first), ctypes.addressof(plan)), "epara_plan_verify_drafts")
     return first, plan

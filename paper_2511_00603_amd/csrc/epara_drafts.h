@@ -26,11 +26,21 @@ EPARA_BOTH int chunks_of_row(int vocab, int dtype, int pieces) { return (pieces_
 struct row_sum { float top; int32_t at; double sum; };     // of a chunk: the largest logit, where it is (greedy sequences only), sum of exp((x - top) / T)
 EPARA_BOTH int64_t rows_items(const epara_verify_args& a, const epara_sequence& s, int chunks) { return static_cast<int64_t>(s.rows) * chunks * (a.draft_logits ? 2 : 1); }
 
-// The second kernel has a workgroup for each chunk of one row of each sequence, and so has the third.
-struct chunk_sum { double p, q, rest; };                   // of the weights of p, of q, and of max(p - q, 0)
-struct drawn_row { int32_t row; float top_p, top_q; int32_t reserved; };         // behind which the third kernel draws a token; -1: it need not
+// The second kernel, a workgroup to a sequence, leaves what the third has to know: the row behind which a token is drawn.
+struct drawn_row {
+    const void* p;                                         // its logits; NULL: nothing is left to draw
+    const void* q;                                         // draft logits: the token comes from max(p - q, 0); else NULL
+    double unit;                                           // weights are 2^((x - top) unit)
+    double top_p, top_q, ratio;                            // ratio: sum of p's weights by sum of q's, as the first kernel has them
+    int32_t vocab, n_without;
+    float uniform;
+    int32_t reserved;
+    int32_t without[TREE_ROWS];                            // tokens that are left out
+};
+// The third has `chunks` workgroups for each sequence, as many as the largest vocabulary needs; with draw_pieces as `pieces` above.
+struct chunk_sum { double p, q, rest, q_of_rest; };        // of a chunk: sums of p, of q, of max(p - ratio q, 0), and of q where that is not 0
 
-// Workspace: a counter per sequence, drawn_row of each, then the first kernel's sums, then chunk_sum of each workgroup of the second.
+// Workspace: a counter per sequence, drawn_row of each, then the first kernel's sums, then chunk_sum of each workgroup of the third.
 EPARA_BOTH int64_t counter_bytes(int n_seqs) { return (static_cast<int64_t>(n_seqs) * 4 + 255) & ~static_cast<int64_t>(255); }
 
 }  // namespace epara_drafts

@@ -58,29 +58,25 @@ int32_t check_verify(const epara_verify_args* args, int32_t G, const epara_seque
     return EPARA_OK;
 }
 
-int32_t count_verify(const epara_verify_args* args, const epara_sequence_table* t, int32_t dtype, int32_t pieces, int32_t* first, const int32_t* expected, int32_t n_items[2])
+// The plan's numbers for its `pieces` and `draw_pieces`, and the running sums.
+int32_t count_verify(const epara_verify_args* args, const epara_sequence_table* t, int32_t dtype, int32_t* first, const int32_t* expected, epara_verify_plan* plan)
 {
-    int64_t items[2] = {0, 0};
+    int64_t items = 0;
+    plan->draw_chunks = 1;
     for (int32_t i = 0; i <= t->n_seqs; ++i) {
-        for (int k = 0; k < 2; ++k) {
-            if (first) first[k * (t->n_seqs + 1) + i] = static_cast<int32_t>(items[k]);
-            if (expected && expected[k * (t->n_seqs + 1) + i] != items[k]) return EPARA_ERR_SHAPE;
-        }
+        if (first) first[i] = static_cast<int32_t>(items);
+        if (expected && expected[i] != items) return EPARA_ERR_SHAPE;
         if (i == t->n_seqs) break;
         const epara_sequence& s = t->h_seqs[i];
-        const int chunks = chunks_of_row(args[s.service].vocab, dtype, pieces);
-        items[0] += rows_items(args[s.service], s, chunks);
-        items[1] += chunks;
-        if (items[0] > INT32_MAX / 256 || items[1] > INT32_MAX / 256) return EPARA_ERR_CAPACITY;
+        const int32_t vocab = args[s.service].vocab;
+        items += rows_items(args[s.service], s, chunks_of_row(vocab, dtype, plan->pieces));
+        plan->draw_chunks = std::max(plan->draw_chunks, chunks_of_row(vocab, dtype, plan->draw_pieces));
+        if (items > INT32_MAX / 256 || static_cast<int64_t>(t->n_seqs) * plan->draw_chunks > INT32_MAX / 256) return EPARA_ERR_CAPACITY;
     }
-    n_items[0] = static_cast<int32_t>(items[0]);
-    n_items[1] = static_cast<int32_t>(items[1]);
+    plan->n_items = static_cast<int32_t>(items);
+    plan->workspace_bytes = counter_bytes(t->n_seqs) + static_cast<int64_t>(t->n_seqs) * sizeof(drawn_row) + items * sizeof(row_sum) +
+                            static_cast<int64_t>(t->n_seqs) * plan->draw_chunks * sizeof(chunk_sum);
     return EPARA_OK;
-}
-
-int64_t verify_workspace(int32_t n_seqs, const int32_t n_items[2]) 
-{
-    return counter_bytes(n_seqs) + static_cast<int64_t>(n_seqs) * sizeof(drawn_row) + static_cast<int64_t>(n_items[0]) * sizeof(row_sum) + static_cast<int64_t>(n_items[1]) * sizeof(chunk_sum);
 }
 
 }  // namespace
@@ -90,13 +86,13 @@ int32_t epara_check_verify_call(const epara_verify_launch& l)
     if (const int32_t rc = check_verify(l.h_args, l.G, &l.table, l.dtype)) return rc;
     if (l.table.n_seqs == 0) return EPARA_OK;
     if (!l.h_first || !l.d_kept || !l.d_next || !l.d_workspace) return EPARA_ERR_NULL;
-    const int32_t p = l.plan.pieces;
-    if (p != 1 && p != 2 && p != 4 && p != 8) return EPARA_ERR_SHAPE;
-    int32_t n[2];
-    if (const int32_t rc = count_verify(l.h_args, &l.table, l.dtype, p, nullptr, l.h_first, n)) return rc;
-    if (n[0] != l.plan.n_items[0] || n[1] != l.plan.n_items[1]) return EPARA_ERR_SHAPE;
+    epara_verify_plan plan = l.plan;
+    const int32_t p = plan.pieces, d = plan.draw_pieces;
+    if ((p != 1 && p != 2 && p != 4 && p != 8) || (d != 1 && d != 2 && d != 4)) return EPARA_ERR_SHAPE;
+    if (const int32_t rc = count_verify(l.h_args, &l.table, l.dtype, nullptr, l.h_first, &plan)) return rc;
+    if (plan.n_items != l.plan.n_items || plan.draw_chunks != l.plan.draw_chunks) return EPARA_ERR_SHAPE;
     if (misaligned(l.d_temperatures, 4) || misaligned(l.d_kept, 4) || misaligned(l.d_next, 4) || misaligned(l.d_workspace, 256)) return EPARA_ERR_ALIGN;
-    if (l.workspace_bytes < verify_workspace(l.table.n_seqs, n)) return EPARA_ERR_CAPACITY;
+    if (l.workspace_bytes < plan.workspace_bytes) return EPARA_ERR_CAPACITY;
     return check_rows_once(l.h_args, &l.table, [](const epara_verify_args&) { return true; });
 }
 
@@ -163,15 +159,15 @@ extern "C" int32_t epara_plan_verify_drafts(const epara_verify_args* h_args, int
     if (const int32_t rc = check_verify(h_args, G, table, dtype)) return rc;
     if (!first || !plan) return EPARA_ERR_NULL;
     if (n_compute_units < 1 || n_compute_units > 65536) return EPARA_ERR_SHAPE;
-    int64_t pieces = 0;                                    // of 16 bytes in all rows
+    int64_t pieces = 0, draws = 0;                         // of 16 bytes in all rows, and in one of each sequence
     for (int32_t i = 0; i < table->n_seqs; ++i) {
         const epara_verify_args& a = h_args[table->h_seqs[i].service];
         pieces += rows_items(a, table->h_seqs[i], 1) * pieces_of_row(a.vocab, dtype);
+        draws += pieces_of_row(a.vocab, dtype);
     }
     *plan = {};
-    plan->pieces = 1;
+    plan->pieces = plan->draw_pieces = 1;
     while (plan->pieces < 8 && pieces >= static_cast<int64_t>(n_compute_units) * 8 * 256 * plan->pieces) plan->pieces *= 2;
-    if (const int32_t rc = count_verify(h_args, table, dtype, plan->pieces, first, nullptr, plan->n_items)) return rc;
-    plan->workspace_bytes = verify_workspace(table->n_seqs, plan->n_items);
-    return EPARA_OK;
+    while (plan->draw_pieces < 4 && draws >= static_cast<int64_t>(n_compute_units) * 4 * 256 * plan->draw_pieces) plan->draw_pieces *= 2;
+    return count_verify(h_args, table, dtype, first, nullptr, plan);
 }

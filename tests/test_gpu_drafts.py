@@ -425,7 +425,7 @@ def test_tokens_are_drawn_with_the_targets_probabilities():
     s.u[:] = (np.arange(n) + 0.5) / n
     plan = run_verify([s])
     got = np.bincount(plan.next.cpu().numpy(), minlength=V)
-    assert np.abs(got - DR.distribution(x, 0.9 if False else float(np.float32(0.9))) * n).max() <= 1.0 + 1e-6
+    assert np.abs(got - DR.distribution(x, float(np.float32(0.9))) * n).max() <= 1.0 + 1e-6
 
 
 def test_every_cut_of_the_rows_gives_the_same():
@@ -434,28 +434,24 @@ def test_every_cut_of_the_rows_gives_the_same():
     s = [Verify(rng, [random_tree(rng, 9), list(range(-1, 4))], 20011, drawn=d, shift=d) for d in (False, True)]
     plan = run_verify(s)
     table, ts = plan.table, plan.temperatures
-    for pieces in (1, 2, 4, 8):
-        for dtype in ("bf16",):
-            counts = [0, 0]
-            first = np.zeros((2, len(table.seqs) + 1), dtype=np.int32)
-            for i, q in enumerate(table.seqs):
-                a = plan.args[q["service"]]
-                chunks = -(-((int(a["vocab"]) - 1 + 7) // 8 + 1) // (256 * pieces))
-                first[:, i] = counts
-                counts[0] += int(q["rows"]) * chunks * (2 if a["draft_logits"] else 1)
-                counts[1] += chunks
-            first[:, -1] = counts
-            own = B.VerifyPlan((B.ctypes.c_int32 * 2)(*counts), pieces, 0, 1 << 20)
-            ws = torch.zeros(1 << 20, dtype=torch.uint8, device=DEV)
-            d_first = R._upload(first, DEV)
-            launch = B.VerifyLaunch(plan.args.ctypes.data, plan.d_args.data_ptr(), first.ctypes.data, d_first.data_ptr(), ts.data_ptr(), plan.kept.data_ptr(), plan.next.data_ptr(),
-                                    ws.data_ptr(), ws.numel(), table.c, own, len(plan.args), plan.dtype)
-            for _ in range(2):
-                plan.kept.fill_(-1)
-                plan.next.fill_(-1)
-                B.epara_verify_drafts(launch, R.current_stream_handle())
-                sync()
-                check_verify(s, plan)
+    for pieces, draw in ((1, 1), (2, 4), (4, 2), (8, 1), (1, 4)):
+        first, at, chunks = np.zeros_like(plan.first), 0, lambda a, n: -(-((int(a["vocab"]) - 1 + 7) // 8 + 1) // (256 * n))
+        for i, q in enumerate(table.seqs):
+            a = plan.args[q["service"]]
+            first[i] = at
+            at += int(q["rows"]) * chunks(a, pieces) * (2 if a["draft_logits"] else 1)
+        first[-1] = at
+        own = B.VerifyPlan(at, pieces, max(chunks(a, draw) for a in plan.args), draw, 1 << 20)
+        ws = torch.zeros(1 << 20, dtype=torch.uint8, device=DEV)
+        d_first = R._upload(first, DEV)
+        launch = B.VerifyLaunch(plan.args.ctypes.data, plan.d_args.data_ptr(), first.ctypes.data, d_first.data_ptr(), ts.data_ptr(), plan.kept.data_ptr(), plan.next.data_ptr(),
+                                ws.data_ptr(), ws.numel(), table.c, own, len(plan.args), plan.dtype)
+        for _ in range(2):
+            plan.kept.fill_(-1)
+            plan.next.fill_(-1)
+            B.epara_verify_drafts(launch, R.current_stream_handle())
+            sync()
+            check_verify(s, plan)
 
 
 # ---- keeping -----------------------------------------------------------------------------------------------------
