@@ -84,13 +84,13 @@ __device__ __forceinline__ row_view view_of(const void* row, int vocab)
 }
 
 // The elements of pieces first, first + step, ..; what is not the row's is -infinity.
-template <int SIZE, int U>
+template <int SIZE, int U, int HINT = 0>
 __device__ __forceinline__ void load_pieces(const row_view& v, int first, int step, float* x)
 {
     constexpr int PER = 16 / SIZE;
     v4i raw[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) raw[u] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(v.rsrc, (first + u * step) * 16, 0, 0));
+    for (int u = 0; u < U; ++u) raw[u] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(v.rsrc, (first + u * step) * 16, 0, HINT));
 #pragma unroll
     for (int u = 0; u < U; ++u) {
 #pragma unroll
@@ -368,7 +368,7 @@ __device__ __forceinline__ row_sum row_chunk(const epara_verify_args& a, const e
     }
     const row_view v = view_of<SIZE>(row_at(draft ? a.draft_logits : a.logits, s.first_row + row, draft ? a.draft_stride : a.stride, SIZE), a.vocab);
     float x[N];
-    load_pieces<SIZE, U>(v, chunk * (NT * U) + tid, NT, x);
+    load_pieces<SIZE, U, 2>(v, chunk * (NT * U) + tid, NT, x);
     float top = x[0];
 #pragma unroll
     for (int j = 1; j < N; ++j) top = fmaxf(top, x[j]);
