@@ -1042,14 +1042,37 @@ typedef struct {
  * ERR_ALIGN; ERR_CAPACITY (no host memory). */
 int32_t epara_draft_trees(const epara_tree_args* h_args, const epara_tree_args* d_args, int32_t G, const epara_sequence_table* table, void* stream);
 
+/* How epara_tree_attention is cut into work: made by epara_plan_tree_attention.  Sequences are of three kinds, by their rows to a key head: up to 32, up to mid_rows, more;
+ * first[k * (n_seqs + 1) .. k * (n_seqs + 1) + n_seqs] are the running sums of the workgroups of kind k. */
+typedef struct {
+    int32_t n_items[3];
+    int32_t part_pages[3];      /* pages to a workgroup: a longer context is cut into parts */
+    int32_t mid_rows, reserved;
+    int64_t workspace_bytes;    /* 0: nothing is cut */
+} epara_tree_attn_plan;
+
+typedef struct {
+    const epara_cache_attn_args* h_args;
+    const epara_cache_attn_args* d_args;
+    const epara_tree_args* h_trees;
+    const epara_tree_args* d_trees;
+    const int32_t* h_first;     /* int32[3 * (n_seqs + 1)] */
+    const int32_t* d_first;
+    void*   d_workspace;        /* as of epara_cache_attn_launch */
+    int64_t workspace_bytes;
+    epara_sequence_table table;
+    epara_tree_attn_plan plan;
+    int32_t G, reserved;
+} epara_tree_attn_launch;
+
 /* epara_cache_attention for sequences whose new rows are trees: with d(i) the number of rows that row i of a sequence follows, it is at position start + d(i) and sees
  * the tokens 0 .. start - 1 (window: those > start + d(i) - window), the rows that it follows, and itself.  A row that is not there gets zeros.  The arithmetic is
- * epara_cache_attention's; workspace, launch and errors too.  trees[g].visible NULL: that service's sequences are no trees (causal, as in
+ * epara_cache_attention's, and so are the errors.  trees[g].visible NULL: that service's sequences are no trees (causal, as in
  * epara_cache_attention), and so are sequences of more than EPARA_TREE_MAX_ROWS rows.  parents and positions are not looked at.
  * Also ERR_SHAPE: a tree that starts before position 0, or has more rows than a window; trees[g].rows other than the service's. */
 int32_t epara_plan_tree_attention(const epara_cache_attn_args* h_args, const epara_tree_args* h_trees, int32_t G, const epara_sequence_table* table, int32_t n_compute_units,
-                                  int32_t* first, epara_cache_attn_plan* plan);
-int32_t epara_tree_attention(const epara_cache_attn_launch* launch, const epara_tree_args* h_trees, const epara_tree_args* d_trees, void* stream);
+                                  int32_t* first, epara_tree_attn_plan* plan);
+int32_t epara_tree_attention(const epara_tree_attn_launch* launch, void* stream);
 
 /* One service's part of epara_verify_drafts.  72 bytes. */
 typedef struct {

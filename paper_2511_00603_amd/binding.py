@@ -120,6 +120,19 @@ class CacheAttnLaunch(ctypes.Structure):
                 ("G", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class TreeAttnPlan(ctypes.Structure):
+    """struct epara_tree_attn_plan."""
+    _fields_ = [("n_items", ctypes.c_int32 * 3), ("part_pages", ctypes.c_int32 * 3), ("mid_rows", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("workspace_bytes", ctypes.c_int64)]
+
+
+class TreeAttnLaunch(ctypes.Structure):
+    """struct epara_tree_attn_launch."""
+    _fields_ = [("h_args", ctypes.c_void_p), ("d_args", ctypes.c_void_p), ("h_trees", ctypes.c_void_p), ("d_trees", ctypes.c_void_p), ("h_first", ctypes.c_void_p),
+                ("d_first", ctypes.c_void_p), ("d_workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64), ("table", SequenceTable), ("plan", TreeAttnPlan),
+                ("G", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 class VerifyPlan(ctypes.Structure):
     """struct epara_verify_plan."""
     _fields_ = [("n_items", ctypes.c_int32), ("pieces", ctypes.c_int32), ("draw_chunks", ctypes.c_int32), ("draw_pieces", ctypes.c_int32), ("workspace_bytes", ctypes.c_int64)]
@@ -283,7 +296,7 @@ def lib():
         L.epara_pages_compact.argtypes = [vp, vp, i32, vp, i32, vp]
         L.epara_draft_trees.argtypes = [vp, vp, i32, vp, vp]
         L.epara_plan_tree_attention.argtypes = [vp, vp, i32, vp, i32, vp, vp]
-        L.epara_tree_attention.argtypes = [vp, vp, vp, vp]
+        L.epara_tree_attention.argtypes = [vp, vp]
         L.epara_plan_verify_drafts.argtypes = [vp, i32, vp, i32, i32, vp, vp]
         L.epara_verify_drafts.argtypes = [vp, vp]
         L.epara_cache_keep.argtypes = [vp, vp, i32, vp, vp, vp]
@@ -436,20 +449,19 @@ def epara_draft_trees(h_args, d_args, table, stream=0):
 
 
 def epara_plan_tree_attention(h_args, h_trees, table, n_compute_units):
-    """h_args: CACHE_ATTN_ARGS[G], h_trees: TREE_ARGS[G] -> (running sums int32[2 (n_seqs + 1)], CacheAttnPlan)."""
+    """h_args: CACHE_ATTN_ARGS[G], h_trees: TREE_ARGS[G] -> (running sums int32[3 (n_seqs + 1)], TreeAttnPlan)."""
     h_args, h_trees = np.ascontiguousarray(h_args, dtype=CACHE_ATTN_ARGS), np.ascontiguousarray(h_trees, dtype=TREE_ARGS)
     if len(h_args) != len(h_trees):
         raise ValueError("%d services, trees of %d" % (len(h_args), len(h_trees)))
-    first, plan = np.zeros(2 * (table.n_seqs + 1), dtype=np.int32), CacheAttnPlan()
+    first, plan = np.zeros(3 * (table.n_seqs + 1), dtype=np.int32), TreeAttnPlan()
     _check(lib().epara_plan_tree_attention(_ptr(h_args) if len(h_args) else None, _ptr(h_trees) if len(h_trees) else None, len(h_args), ctypes.addressof(table),
                                            int(n_compute_units), _ptr(first), ctypes.addressof(plan)), "epara_plan_tree_attention")
     return first, plan
 
 
-def epara_tree_attention(launch, h_trees, d_trees, stream=0):
-    """launch: a CacheAttnLaunch, h_trees: TREE_ARGS[G] (kept alive, with what they point to, by the caller); d_trees: device address of the same bytes."""
-    h_trees = np.ascontiguousarray(h_trees, dtype=TREE_ARGS)
-    _check(lib().epara_tree_attention(ctypes.addressof(launch), _ptr(h_trees) if len(h_trees) else None, int(d_trees) or None, int(stream) or None), "epara_tree_attention")
+def epara_tree_attention(launch, stream=0):
+    """launch: a TreeAttnLaunch (kept alive, with what it points to, by the caller)."""
+    _check(lib().epara_tree_attention(ctypes.addressof(launch), int(stream) or None), "epara_tree_attention")
 
 
 def epara_plan_verify_drafts(h_args, table, dtype, n_compute_units):

@@ -19,7 +19,7 @@ UNITS = ["epara_k_bf16_plain.hip", "epara_k_bf16_gated.hip", "epara_k_fp8_plain.
 SOURCES = [os.path.join(CSRC, u) for u in UNITS]
 HEADERS = [os.path.join(ROOT, "include", "epara.h")] + [os.path.join(CSRC, h) for h in (
     "epara_cast.h", "epara_device.h", "epara_internal.h", "epara_plan.h", "epara_panel.h", "epara_block_tile.h", "epara_half.h", "epara_stream.h", "epara_f32.h", "epara_grouped.h", "epara_rows.h",
-    "epara_cache.h", "epara_cache_device.h", "epara_cache_host.h", "epara_cache_checks.h", "epara_drafts.h")]
+    "epara_cache.h", "epara_cache_device.h", "epara_cache_host.h", "epara_cache_checks.h", "epara_attend_mid.h", "epara_drafts.h")]
 LIB = os.path.join(HERE, "libepara.so")
 OBJ_DIR = os.path.join(ROOT, "_build", "obj")
 

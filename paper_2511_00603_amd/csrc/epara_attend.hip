@@ -42,8 +42,10 @@
 #include "epara_cache.h"
 #include "epara_cache_device.h"
 #include "epara_cache_host.h"
+#include "epara_drafts.h"
 
 using namespace epara_cache;
+using namespace epara_drafts;
 
 namespace {
 
@@ -388,7 +390,7 @@ __device__ __forceinline__ void join_few(const work_item& w, char* slots, few_ld
     }
 }
 
-template <int D, bool TREE>
+template <int D>
 __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __restrict__ pages, uint32_t* counters, char* slots, char* lds_bytes, int item)
 {
     few_lds<D>& lds = *reinterpret_cast<few_lds<D>*>(lds_bytes);
@@ -399,17 +401,9 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
 
     // ---- my row: a token and a query head
     const int row = min_of(w.tile * FEW_TILE + n, w.rows - 1), token = row / w.group, query_head = w.head * w.group + row - token * w.group;
+    const int last_key = w.s.start + token, first_key = a.window > 0 ? last_key - a.window + 1 : 0;
+    const int low_token = w.s.start + w.tile * FEW_TILE / w.group, high_token = w.s.start + (min_of(w.rows, w.tile * FEW_TILE + FEW_TILE) - 1) / w.group;
     const int end = w.s.start + w.s.rows;                  // tokens in the cache
-    const bool tree = TREE && w.visible;
-    tree_row bits = {};
-    int last_key = w.s.start + token, low_token = w.s.start + w.tile * FEW_TILE / w.group;       // pages up to low_token are seen by all rows of the tile
-    const int high_token = w.s.start + (min_of(w.rows, w.tile * FEW_TILE + FEW_TILE) - 1) / w.group;
-    if (tree) {
-        bits = tree_row_of(w, token);
-        last_key = w.s.start + bits.follows;               // its position
-        low_token = __ballot(!bits.there) ? -1 : w.s.start - 1;
-    }
-    const int first_key = a.window > 0 ? last_key - a.window + 1 : 0;
 
     // ---- the query: dims 16 q .. and (heads of 128) 64 + 16 q .., 8 to an instruction
     v8h query[KS][2];
@@ -506,21 +500,13 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
             unit = 1.f;
         }
         if (p * PAGE + PAGE - 1 > low_token || (a.window > 0 && p * PAGE <= high_token - a.window)) {
-            if (tree) {
-                const uint32_t seen = static_cast<uint32_t>(seen_of_page(bits, p * PAGE - w.s.start) >> (16 * q));
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
+            for (int t = 0; t < 4; ++t)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) z[t][i] = !(seen >> (4 * t + i) & 1) || at + 4 * t + i < first_key ? -INFINITY : z[t][i] * unit;
-            } else {
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int key = at + 4 * t + i;
-                        z[t][i] = key > last_key || key < first_key ? -INFINITY : z[t][i] * unit;
-                    }
-            }
+                for (int i = 0; i < 4; ++i) {
+                    const int key = at + 4 * t + i;
+                    z[t][i] = key > last_key || key < first_key ? -INFINITY : z[t][i] * unit;
+                }
             unit = 1.f;
         }
         // ---- the row's largest score here: mine are 16 keys of one block, the lanes n, n + 16, .. hold the others
@@ -631,17 +617,16 @@ __device__ __forceinline__ void attend_few(const work_item& w, const int32_t* __
     for (int j = 0; j < COLS; j += 4) store_out4(w, out_row, c + j, scaled4(v4f{oo[j], oo[j + 1], oo[j + 2], oo[j + 3]} * inv, static_cast<int>(vv)));
 }
 
-template <bool TREE>
-__global__ __launch_bounds__(NT, 2) void attend_few_kernel(const epara_cache_attn_args* __restrict__ args, const epara_tree_args* __restrict__ trees,
-                                                          const epara_sequence* __restrict__ seqs, const int32_t* __restrict__ pages, const int32_t* __restrict__ first,
-                                                          int n_seqs, int part_pages, uint32_t* counters, char* slots)
+__global__ __launch_bounds__(NT, 2) void attend_few_kernel(const epara_cache_attn_args* __restrict__ args, const epara_sequence* __restrict__ seqs,
+                                                          const int32_t* __restrict__ pages, const int32_t* __restrict__ first, int n_seqs, int part_pages,
+                                                          uint32_t* counters, char* slots)
 {
     __shared__ __attribute__((aligned(16))) char lds[sizeof(few_lds<128>)];
     const int item = blockIdx.x;
-    const work_item w = find_work<FEW_TILE, TREE>(args, trees, seqs, first, n_seqs, part_pages, item, threadIdx.x & 63);
+    const work_item w = find_work<FEW_TILE, false>(args, nullptr, seqs, first, n_seqs, part_pages, item, threadIdx.x & 63);
     if (w.part > 0 && w.part >= w.parts) return;           // this tile has fewer parts than the sequence's longest
-    if (w.a.head_dim == 128) attend_few<128, TREE>(w, pages, counters, slots, lds, item);
-    else                     attend_few<64, TREE>(w, pages, counters, slots, lds, item);
+    if (w.a.head_dim == 128) attend_few<128>(w, pages, counters, slots, lds, item);
+    else                     attend_few<64>(w, pages, counters, slots, lds, item);
 }
 
 // ---- many rows -------------------------------------------------------------------------------------------------
@@ -972,22 +957,14 @@ __global__ __launch_bounds__(NT, 2) void attend_many_kernel(const epara_cache_at
     else                     attend_many<64, TREE>(w, pages, counters, slots, (ldsptr)ring, item);
 }
 
-template <bool TREE>
-int32_t launch_attention(const epara_cache_attn_launch& l, const epara_tree_args* d_trees, const bool cut[2], void* stream)
+#include "epara_attend_mid.h"
+
+template <bool ONCE>
+void launch_mid(const epara_tree_attn_launch& l, int kind, uint32_t* counters, char* slots, hipStream_t s)
 {
-    if (l.plan.n_items[0] + l.plan.n_items[1] == 0 || l.table.n_seqs == 0) return EPARA_OK;
-    if (!l.d_args || !l.d_first || (TREE && !d_trees)) return EPARA_ERR_NULL;
-    uint32_t* counters = static_cast<uint32_t*>(l.d_workspace);
-    char* slots = static_cast<char*>(l.d_workspace) + epara_attn_counter_bytes(l.plan.n_items);
-    char* many_slots = slots + (cut[0] ? static_cast<size_t>(l.plan.n_items[0]) * FEW_TILE * SLOT_FLOATS * 4 : 0);
-    hipStream_t s = static_cast<hipStream_t>(stream);
-    if (l.plan.n_items[1] > 0)
-        hipLaunchKernelGGL(attend_many_kernel<TREE>, dim3(static_cast<unsigned>(l.plan.n_items[1])), dim3(NT), 0, s, l.d_args, d_trees, l.table.d_seqs, l.table.d_pages,
-                           l.d_first + l.table.n_seqs + 1, l.table.n_seqs, l.plan.part_pages[1], counters + l.plan.n_items[0], many_slots);
-    if (l.plan.n_items[0] > 0)
-        hipLaunchKernelGGL(attend_few_kernel<TREE>, dim3(static_cast<unsigned>(l.plan.n_items[0])), dim3(NT), 0, s, l.d_args, d_trees, l.table.d_seqs, l.table.d_pages, l.d_first,
-                           l.table.n_seqs, l.plan.part_pages[0], counters, slots);
-    return hipGetLastError() == hipSuccess ? EPARA_OK : EPARA_ERR_HIP;
+    if (l.plan.n_items[kind] == 0) return;
+    hipLaunchKernelGGL(attend_mid_kernel<ONCE>, dim3(static_cast<unsigned>(l.plan.n_items[kind])), dim3(NT), 0, s, l.d_args, l.d_trees, l.table.d_seqs, l.table.d_pages,
+                       l.d_first + kind * (l.table.n_seqs + 1), l.table.n_seqs, l.plan.part_pages[kind], counters, slots);
 }
 
 }  // namespace
@@ -997,17 +974,43 @@ extern "C" {
 int32_t epara_cache_attention(const epara_cache_attn_launch* launch, void* stream)
 {
     if (!launch) return EPARA_ERR_NULL;
+    const epara_cache_attn_launch& l = *launch;
     bool cut[2];
-    if (const int32_t rc = epara_check_attn_call(*launch, cut)) return rc;
-    return launch_attention<false>(*launch, nullptr, cut, stream);
+    if (const int32_t rc = epara_check_attn_call(l, cut)) return rc;
+    if (l.plan.n_items[0] + l.plan.n_items[1] == 0 || l.table.n_seqs == 0) return EPARA_OK;
+    if (!l.d_args || !l.d_first) return EPARA_ERR_NULL;
+    uint32_t* counters = static_cast<uint32_t*>(l.d_workspace);
+    char* slots = static_cast<char*>(l.d_workspace) + epara_attn_counter_bytes(l.plan.n_items);
+    char* many_slots = slots + (cut[0] ? static_cast<size_t>(l.plan.n_items[0]) * FEW_TILE * SLOT_FLOATS * 4 : 0);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (l.plan.n_items[1] > 0)
+        hipLaunchKernelGGL(attend_many_kernel<false>, dim3(static_cast<unsigned>(l.plan.n_items[1])), dim3(NT), 0, s, l.d_args, nullptr, l.table.d_seqs, l.table.d_pages,
+                           l.d_first + l.table.n_seqs + 1, l.table.n_seqs, l.plan.part_pages[1], counters + l.plan.n_items[0], many_slots);
+    if (l.plan.n_items[0] > 0)
+        hipLaunchKernelGGL(attend_few_kernel, dim3(static_cast<unsigned>(l.plan.n_items[0])), dim3(NT), 0, s, l.d_args, l.table.d_seqs, l.table.d_pages, l.d_first,
+                           l.table.n_seqs, l.plan.part_pages[0], counters, slots);
+    return hipGetLastError() == hipSuccess ? EPARA_OK : EPARA_ERR_HIP;
 }
 
-int32_t epara_tree_attention(const epara_cache_attn_launch* launch, const epara_tree_args* h_trees, const epara_tree_args* d_trees, void* stream)
+int32_t epara_tree_attention(const epara_tree_attn_launch* launch, void* stream)
 {
-    if (!launch || (launch->G > 0 && !h_trees)) return EPARA_ERR_NULL;
-    bool cut[2];
-    if (const int32_t rc = epara_check_attn_call(*launch, cut, h_trees)) return rc;
-    return launch_attention<true>(*launch, d_trees, cut, stream);
+    if (!launch) return EPARA_ERR_NULL;
+    const epara_tree_attn_launch& l = *launch;
+    bool cut[3];
+    if (const int32_t rc = epara_check_tree_attn_call(l, cut)) return rc;
+    const int32_t* n = l.plan.n_items;
+    if (l.table.n_seqs == 0 || n[0] + n[1] + n[2] == 0) return EPARA_OK;
+    if (!l.d_args || !l.d_first || !l.d_trees) return EPARA_ERR_NULL;
+    const tree_workspace at = tree_workspace_of(n, cut);
+    char* ws = static_cast<char*>(l.d_workspace);
+    uint32_t* counters = reinterpret_cast<uint32_t*>(ws);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (n[2] > 0)
+        hipLaunchKernelGGL(attend_many_kernel<true>, dim3(static_cast<unsigned>(n[2])), dim3(NT), 0, s, l.d_args, l.d_trees, l.table.d_seqs, l.table.d_pages,
+                           l.d_first + 2 * (l.table.n_seqs + 1), l.table.n_seqs, l.plan.part_pages[2], counters + n[0] + n[1], ws + at.slots[2]);
+    launch_mid<false>(l, 1, counters + n[0], ws + at.slots[1], s);
+    launch_mid<true>(l, 0, counters, ws + at.slots[0], s);
+    return hipGetLastError() == hipSuccess ? EPARA_OK : EPARA_ERR_HIP;
 }
 
 }  // extern "C"

@@ -71,6 +71,14 @@ EPARA_BOTH page_range pages_of_rows(const epara_sequence& s, int window, bool tr
 
 // ---- trees of drafted tokens: a sequence of up to EPARA_TREE_MAX_ROWS new rows is one where its service has bits of them
 constexpr int TREE_ROWS = EPARA_TREE_MAX_ROWS, TREE_WORDS = TREE_ROWS / 64;
+// The kinds of sequences of epara_tree_attention, by their rows to a key head: one tile of 32, several of them (up to mid_rows rows), tiles of 128.
+constexpr int MID_TILE = 32, TREE_KINDS = 3;
+EPARA_BOTH int tree_tile(int kind) { return kind < 2 ? MID_TILE : MANY_TILE; }
+EPARA_BOTH int tree_kind(const epara_cache_attn_args& a, const epara_sequence& s, int mid_rows)
+{
+    const int64_t rows = static_cast<int64_t>(s.rows) * (a.heads / a.kv_heads);
+    return rows <= MID_TILE ? 0 : rows <= mid_rows ? 1 : 2;
+}
 EPARA_BOTH bool is_tree(const epara_tree_args* trees, const epara_sequence& s) { return trees && s.rows <= TREE_ROWS && trees[s.service].visible; }
 
 }  // namespace epara_cache

@@ -74,8 +74,10 @@ int32_t count_append(const epara_append_args* args, const epara_sequence_table* 
     return EPARA_OK;
 }
 
+}  // namespace
+
 // trees: of epara_tree_attention, else NULL.
-int32_t check_attn(const epara_cache_attn_args* args, int32_t G, const epara_sequence_table* t, const epara_tree_args* trees)
+int32_t epara_check_attn_args(const epara_cache_attn_args* args, int32_t G, const epara_sequence_table* t, const epara_tree_args* trees)
 {
     if (G < 0) return EPARA_ERR_SHAPE;
     if (G > 0 && !args) return EPARA_ERR_NULL;
@@ -104,6 +106,8 @@ int32_t check_attn(const epara_cache_attn_args* args, int32_t G, const epara_seq
     return EPARA_OK;
 }
 
+namespace {
+
 struct seq_tiles { int few, tiles; };
 seq_tiles tiles_of(const epara_cache_attn_args& a, const epara_sequence& s)
 {
@@ -111,14 +115,14 @@ seq_tiles tiles_of(const epara_cache_attn_args& a, const epara_sequence& s)
     return {few, static_cast<int>(ceil_div(static_cast<int64_t>(s.rows) * (a.heads / a.kv_heads), few ? FEW_TILE : MANY_TILE))};
 }
 
-page_range pages_of_tile(const epara_cache_attn_args& a, const epara_sequence& s, bool tree, int few, int tile)
+page_range pages_of_tile(const epara_cache_attn_args& a, const epara_sequence& s, int few, int tile)
 {
     const int group = a.heads / a.kv_heads, size = few ? FEW_TILE : MANY_TILE, rows = s.rows * group;
-    return pages_of_rows(s, a.window, tree, tile * size / group, (std::min(rows, tile * size + size) - 1) / group);
+    return pages_of_rows(s, a.window, false, tile * size / group, (std::min(rows, tile * size + size) - 1) / group);
 }
 
 // Running sums of workgroups of both kinds of sequences, with parts of part_pages pages.
-int32_t count_attn(const epara_cache_attn_args* args, const epara_sequence_table* t, const epara_tree_args* trees, const int32_t part_pages[2], int32_t* first, const int32_t* expected,
+int32_t count_attn(const epara_cache_attn_args* args, const epara_sequence_table* t, const int32_t part_pages[2], int32_t* first, const int32_t* expected,
                    int32_t n_items[2], bool cut[2])
 {
     int64_t items[2] = {0, 0};
@@ -136,7 +140,7 @@ int32_t count_attn(const epara_cache_attn_args* args, const epara_sequence_table
         const int k = w.few ? 0 : 1;
         int64_t parts = 1;
         for (int tile = 0; tile < w.tiles; ++tile) {
-            const page_range r = pages_of_tile(a, s, is_tree(trees, s), w.few, tile);
+            const page_range r = pages_of_tile(a, s, w.few, tile);
             parts = std::max(parts, ceil_div(r.hi - r.lo, part_pages[k]));
         }
         if (parts > MAX_PARTS) return EPARA_ERR_SHAPE;
@@ -156,32 +160,6 @@ int64_t attn_workspace(const int32_t n_items[2], const bool cut[2])
            (cut[1] ? static_cast<int64_t>(n_items[1]) * MANY_TILE * SLOT_FLOATS * 4 : 0);
 }
 
-int32_t plan_attn(const epara_cache_attn_args* h_args, const epara_tree_args* trees, int32_t G, const epara_sequence_table* table, int32_t n_compute_units,
-                  int32_t* first, epara_cache_attn_plan* plan)
-{
-    if (const int32_t rc = check_attn(h_args, G, table, trees)) return rc;
-    if (!first || !plan) return EPARA_ERR_NULL;
-    if (n_compute_units < 1 || n_compute_units > 65536) return EPARA_ERR_SHAPE;
-    int64_t work[2] = {0, 0}, longest[2] = {0, 0};
-    for (int32_t i = 0; i < table->n_seqs; ++i) {
-        const epara_sequence& s = table->h_seqs[i];
-        const epara_cache_attn_args& a = h_args[s.service];
-        if (s.rows == 0) continue;
-        const seq_tiles w = tiles_of(a, s);
-        const int k = w.few ? 0 : 1;
-        for (int tile = 0; tile < w.tiles; ++tile) {
-            const page_range r = pages_of_tile(a, s, is_tree(trees, s), w.few, tile);
-            work[k] += static_cast<int64_t>(r.hi - r.lo) * a.kv_heads;
-            longest[k] = std::max<int64_t>(longest[k], r.hi - r.lo);
-        }
-    }
-    epara_attn_part_pages(work, longest, n_compute_units, plan->part_pages);
-    bool cut[2];
-    if (const int32_t rc = count_attn(h_args, table, trees, plan->part_pages, first, nullptr, plan->n_items, cut)) return rc;
-    plan->workspace_bytes = attn_workspace(plan->n_items, cut);
-    return EPARA_OK;
-}
-
 }  // namespace
 
 int32_t epara_check_append_call(const epara_append_args* h_args, int32_t G, const epara_sequence_table* table, const int32_t* h_first)
@@ -194,15 +172,15 @@ int32_t epara_check_append_call(const epara_append_args* h_args, int32_t G, cons
     return check_written_once(h_args, table);
 }
 
-int32_t epara_check_attn_call(const epara_cache_attn_launch& l, bool cut[2], const epara_tree_args* trees)
+int32_t epara_check_attn_call(const epara_cache_attn_launch& l, bool cut[2])
 {
-    if (const int32_t rc = check_attn(l.h_args, l.G, &l.table, trees)) return rc;
+    if (const int32_t rc = epara_check_attn_args(l.h_args, l.G, &l.table, nullptr)) return rc;
     cut[0] = cut[1] = false;
     if (l.table.n_seqs == 0) return EPARA_OK;
     if (!l.h_first) return EPARA_ERR_NULL;
     if (l.plan.part_pages[0] < 1 || l.plan.part_pages[1] < 1) return EPARA_ERR_SHAPE;
     int32_t n[2];
-    if (const int32_t rc = count_attn(l.h_args, &l.table, trees, l.plan.part_pages, nullptr, l.h_first, n, cut)) return rc;
+    if (const int32_t rc = count_attn(l.h_args, &l.table, l.plan.part_pages, nullptr, l.h_first, n, cut)) return rc;
     if (n[0] != l.plan.n_items[0] || n[1] != l.plan.n_items[1]) return EPARA_ERR_SHAPE;
     if (const int32_t rc = check_rows_once(l.h_args, &l.table, [](const epara_cache_attn_args&) { return true; })) return rc;
     const int64_t bytes = attn_workspace(n, cut);
@@ -287,14 +265,27 @@ int32_t epara_plan_cache_append(const epara_append_args* h_args, int32_t G, cons
 int32_t epara_plan_cache_attention(const epara_cache_attn_args* h_args, int32_t G, const epara_sequence_table* table, int32_t n_compute_units,
                                    int32_t* first, epara_cache_attn_plan* plan)
 {
-    return plan_attn(h_args, nullptr, G, table, n_compute_units, first, plan);
-}
-
-int32_t epara_plan_tree_attention(const epara_cache_attn_args* h_args, const epara_tree_args* h_trees, int32_t G, const epara_sequence_table* table, int32_t n_compute_units,
-                                  int32_t* first, epara_cache_attn_plan* plan)
-{
-    if (G > 0 && !h_trees) return EPARA_ERR_NULL;
-    return plan_attn(h_args, h_trees, G, table, n_compute_units, first, plan);
+    if (const int32_t rc = epara_check_attn_args(h_args, G, table, nullptr)) return rc;
+    if (!first || !plan) return EPARA_ERR_NULL;
+    if (n_compute_units < 1 || n_compute_units > 65536) return EPARA_ERR_SHAPE;
+    int64_t work[2] = {0, 0}, longest[2] = {0, 0};
+    for (int32_t i = 0; i < table->n_seqs; ++i) {
+        const epara_sequence& s = table->h_seqs[i];
+        const epara_cache_attn_args& a = h_args[s.service];
+        if (s.rows == 0) continue;
+        const seq_tiles w = tiles_of(a, s);
+        const int k = w.few ? 0 : 1;
+        for (int tile = 0; tile < w.tiles; ++tile) {
+            const page_range r = pages_of_tile(a, s, w.few, tile);
+            work[k] += static_cast<int64_t>(r.hi - r.lo) * a.kv_heads;
+            longest[k] = std::max<int64_t>(longest[k], r.hi - r.lo);
+        }
+    }
+    epara_attn_part_pages(work, longest, n_compute_units, plan->part_pages);
+    bool cut[2];
+    if (const int32_t rc = count_attn(h_args, table, plan->part_pages, first, nullptr, plan->n_items, cut)) return rc;
+    plan->workspace_bytes = attn_workspace(plan->n_items, cut);
+    return EPARA_OK;
 }
 
 int32_t epara_page_pool_init(epara_page_pool* pool, int32_t* refs, int32_t* free_pages, int32_t n_pages)

@@ -9,7 +9,8 @@
 #include "epara_plan.h"
 
 EPARA_HIDDEN int32_t epara_check_append_call(const epara_append_args* h_args, int32_t G, const epara_sequence_table* table, const int32_t* h_first);
-EPARA_HIDDEN int32_t epara_check_attn_call(const epara_cache_attn_launch& launch, bool cut[2], const epara_tree_args* trees = nullptr);      // cut: some context of few / many rows is in parts
+EPARA_HIDDEN int32_t epara_check_attn_args(const epara_cache_attn_args* args, int32_t G, const epara_sequence_table* table, const epara_tree_args* trees);      // trees: or NULL
+EPARA_HIDDEN int32_t epara_check_attn_call(const epara_cache_attn_launch& launch, bool cut[2]);      // cut: some context of few / many rows is in parts
 EPARA_HIDDEN int32_t epara_check_copy_call(const epara_page_copy* caches, int32_t G, const epara_page_move* moves, int32_t n_moves, int32_t* n_chunks);
 
 // Workspace of attention: a counter per workgroup of both kinds, padded to 256 bytes, then a slot per workgroup of each kind that is cut.

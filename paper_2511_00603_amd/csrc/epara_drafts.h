@@ -43,9 +43,38 @@ struct chunk_sum { double p, q, rest, q_of_rest; };        // of a chunk: sums o
 // Workspace: a counter per sequence, drawn_row of each, then the first kernel's sums, then chunk_sum of each workgroup of the third.
 EPARA_BOTH int64_t counter_bytes(int n_seqs) { return (static_cast<int64_t>(n_seqs) * 4 + 255) & ~static_cast<int64_t>(255); }
 
+// ---- attention of trees.  Up to MID_ROWS rows to a key head are taken in tiles of 32 (32 trees of 32 with 128 rows to a head: 87 us, tiles of 128: 77), and up to MID_ROWS_ALONE where
+// tiles of 128 would be too few to fill half the compute units (one tree of 64 with 256 rows to a head at 16000 tokens: 41 us, tiles of 128, whose parts take longer to join: 46; 183 rows
+// of heads of 64 at 32768, capped: 32 and 44).
+constexpr int MID_ROWS = 64, MID_ROWS_ALONE = 256;
+
+// Pages to a workgroup: one workgroup (tiles of 128: two) to a compute unit where the work is small.  work: pages x key heads that the tiles of a kind see;
+// longest: pages that one tile sees at most.
+inline int32_t tree_part_pages(int kind, int64_t work, int64_t longest, int32_t n_compute_units)
+{
+    const int64_t slots = (kind == 2 ? 2 : 1) * static_cast<int64_t>(n_compute_units), fewest = kind == 2 ? 16 : 8;
+    const int64_t even = work / slots + 1, part = even < fewest ? fewest : even > 64 ? 64 : even;
+    const int64_t least = (longest + epara_cache::MAX_PARTS - 1) / epara_cache::MAX_PARTS;
+    return static_cast<int32_t>(part < least ? least : part);
+}
+
+// Workspace, where something is cut: a counter for each workgroup, then a slot for each workgroup of the kinds that are cut.
+struct tree_workspace { int64_t slots[3], bytes; };
+inline tree_workspace tree_workspace_of(const int32_t n_items[3], const bool cut[3])
+{
+    const int64_t items = static_cast<int64_t>(n_items[0]) + n_items[1] + n_items[2];
+    tree_workspace w = {{0, 0, 0}, cut[0] || cut[1] || cut[2] ? (items * 4 + 255) & ~static_cast<int64_t>(255) : 0};
+    for (int k = 0; k < 3; ++k) {
+        w.slots[k] = w.bytes;
+        if (cut[k]) w.bytes += static_cast<int64_t>(n_items[k]) * epara_cache::tree_tile(k) * epara_cache::SLOT_FLOATS * 4;
+    }
+    return w;
+}
+
 }  // namespace epara_drafts
 
 EPARA_HIDDEN int32_t epara_check_trees_call(const epara_tree_args* h_args, int32_t G, const epara_sequence_table* table);
+EPARA_HIDDEN int32_t epara_check_tree_attn_call(const epara_tree_attn_launch& launch, bool cut[3]);
 EPARA_HIDDEN int32_t epara_check_verify_call(const epara_verify_launch& launch);
 EPARA_HIDDEN int32_t epara_check_keep_call(const epara_keep_args* h_caches, int32_t n_caches, const epara_sequence_table* table, int32_t* n_items);
 

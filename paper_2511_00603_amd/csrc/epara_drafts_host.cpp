@@ -2,6 +2,7 @@
 #include "epara.h"
 #include "epara_cache.h"
 #include "epara_cache_checks.h"
+#include "epara_cache_host.h"
 #include "epara_drafts.h"
 
 #include <algorithm>
@@ -28,6 +29,101 @@ int32_t epara_check_trees_call(const epara_tree_args* args, int32_t G, const epa
     for (int32_t i = 0; i < t->n_seqs; ++i)
         if (t->h_seqs[i].rows > 0 && t->h_seqs[i].rows <= TREE_ROWS && t->h_seqs[i].start < 0) return EPARA_ERR_SHAPE;
     return check_rows_once(args, t, [](const epara_tree_args&) { return true; });
+}
+
+namespace {
+
+page_range pages_of_tile(const epara_cache_attn_args& a, const epara_sequence& s, bool tree, int size, int tile)
+{
+    const int group = a.heads / a.kv_heads, rows = s.rows * group;
+    return pages_of_rows(s, a.window, tree, tile * size / group, (std::min(rows, tile * size + size) - 1) / group);
+}
+int tiles_of(const epara_cache_attn_args& a, const epara_sequence& s, int size) { return static_cast<int>(ceil_div(static_cast<int64_t>(s.rows) * (a.heads / a.kv_heads), size)); }
+
+// Running sums of the workgroups of the three kinds of sequences, with parts of part_pages pages.
+int32_t count_tree_attn(const epara_cache_attn_args* args, const epara_tree_args* trees, const epara_sequence_table* t, const int32_t part_pages[3], int32_t mid_rows,
+                        int32_t* first, const int32_t* expected, int32_t n_items[3], bool cut[3])
+{
+    int64_t items[TREE_KINDS] = {};
+    for (int k = 0; k < TREE_KINDS; ++k) cut[k] = false;
+    for (int32_t i = 0; i <= t->n_seqs; ++i) {
+        for (int k = 0; k < TREE_KINDS; ++k) {
+            if (first) first[k * (t->n_seqs + 1) + i] = static_cast<int32_t>(items[k]);
+            if (expected && expected[k * (t->n_seqs + 1) + i] != items[k]) return EPARA_ERR_SHAPE;
+        }
+        if (i == t->n_seqs) break;
+        const epara_sequence& s = t->h_seqs[i];
+        const epara_cache_attn_args& a = args[s.service];
+        if (s.rows == 0) continue;
+        const int k = tree_kind(a, s, mid_rows), size = tree_tile(k), tiles = tiles_of(a, s, size);
+        int64_t parts = 1;
+        for (int tile = 0; tile < tiles; ++tile) {
+            const page_range r = pages_of_tile(a, s, is_tree(trees, s), size, tile);
+            parts = std::max(parts, ceil_div(r.hi - r.lo, part_pages[k]));
+        }
+        if (parts > MAX_PARTS) return EPARA_ERR_SHAPE;
+        cut[k] = cut[k] || parts > 1;
+        items[k] += parts * tiles * a.kv_heads;
+        if (items[k] > INT32_MAX / 256) return EPARA_ERR_CAPACITY;
+    }
+    for (int k = 0; k < TREE_KINDS; ++k) n_items[k] = static_cast<int32_t>(items[k]);
+    return EPARA_OK;
+}
+
+}  // namespace
+
+int32_t epara_check_tree_attn_call(const epara_tree_attn_launch& l, bool cut[3])
+{
+    if (l.G > 0 && !l.h_trees) return EPARA_ERR_NULL;
+    if (const int32_t rc = epara_check_attn_args(l.h_args, l.G, &l.table, l.h_trees)) return rc;
+    if (l.table.n_seqs == 0) return EPARA_OK;
+    if (!l.h_first) return EPARA_ERR_NULL;
+    for (int k = 0; k < TREE_KINDS; ++k)
+        if (l.plan.part_pages[k] < 1) return EPARA_ERR_SHAPE;
+    int32_t n[TREE_KINDS];
+    if (const int32_t rc = count_tree_attn(l.h_args, l.h_trees, &l.table, l.plan.part_pages, l.plan.mid_rows, nullptr, l.h_first, n, cut)) return rc;
+    if (!std::equal(n, n + TREE_KINDS, l.plan.n_items)) return EPARA_ERR_SHAPE;
+    if (const int32_t rc = check_rows_once(l.h_args, &l.table, [](const epara_cache_attn_args&) { return true; })) return rc;
+    const int64_t bytes = tree_workspace_of(n, cut).bytes;
+    if (bytes > 0) {
+        if (!l.d_workspace) return EPARA_ERR_NULL;
+        if (misaligned(l.d_workspace, 256)) return EPARA_ERR_ALIGN;
+        if (l.workspace_bytes < bytes) return EPARA_ERR_CAPACITY;
+    }
+    return EPARA_OK;
+}
+
+extern "C" int32_t epara_plan_tree_attention(const epara_cache_attn_args* h_args, const epara_tree_args* h_trees, int32_t G, const epara_sequence_table* table, int32_t n_compute_units,
+                                             int32_t* first, epara_tree_attn_plan* plan)
+{
+    if (G > 0 && !h_trees) return EPARA_ERR_NULL;
+    if (const int32_t rc = epara_check_attn_args(h_args, G, table, h_trees)) return rc;
+    if (!first || !plan) return EPARA_ERR_NULL;
+    if (n_compute_units < 1 || n_compute_units > 65536) return EPARA_ERR_SHAPE;
+    *plan = {};
+    int64_t many = 0;                                      // tiles of 128 that a rule by rows alone would give
+    for (int32_t i = 0; i < table->n_seqs; ++i) {
+        const epara_cache_attn_args& a = h_args[table->h_seqs[i].service];
+        if (tree_kind(a, table->h_seqs[i], MID_ROWS) == 2) many += static_cast<int64_t>(tiles_of(a, table->h_seqs[i], MANY_TILE)) * a.kv_heads;
+    }
+    plan->mid_rows = many < n_compute_units / 2 ? MID_ROWS_ALONE : MID_ROWS;
+    int64_t work[TREE_KINDS] = {}, longest[TREE_KINDS] = {};
+    for (int32_t i = 0; i < table->n_seqs; ++i) {
+        const epara_sequence& s = table->h_seqs[i];
+        const epara_cache_attn_args& a = h_args[s.service];
+        if (s.rows == 0) continue;
+        const int k = tree_kind(a, s, plan->mid_rows), size = tree_tile(k), tiles = tiles_of(a, s, size);
+        for (int tile = 0; tile < tiles; ++tile) {
+            const page_range r = pages_of_tile(a, s, is_tree(h_trees, s), size, tile);
+            work[k] += static_cast<int64_t>(r.hi - r.lo) * a.kv_heads;
+            longest[k] = std::max<int64_t>(longest[k], r.hi - r.lo);
+        }
+    }
+    for (int k = 0; k < TREE_KINDS; ++k) plan->part_pages[k] = tree_part_pages(k, work[k], longest[k], n_compute_units);
+    bool cut[TREE_KINDS];
+    if (const int32_t rc = count_tree_attn(h_args, h_trees, table, plan->part_pages, plan->mid_rows, first, nullptr, plan->n_items, cut)) return rc;
+    plan->workspace_bytes = tree_workspace_of(plan->n_items, cut).bytes;
+    return EPARA_OK;
 }
 
 namespace {

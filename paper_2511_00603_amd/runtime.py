@@ -423,66 +423,69 @@ def cache_append(plan, stream=None):
     plan._call(_stream_of_call() if stream is None else stream)
 
 
+def _attn_args(table, groups):
+    """CACHE_ATTN_ARGS of the services of a table."""
+    if len(groups) != table.G:
+        raise ValueError("%d services in the table, %d groups" % (table.G, len(groups)))
+    args, bf = np.zeros(len(groups), dtype=B.CACHE_ATTN_ARGS), torch.bfloat16
+    for i, g in enumerate(groups):
+        c, H = g["cache"], int(g["heads"])
+        rows, D = int(g["Q"].shape[0]), c.head_dim
+        args[i] = (_want(g["Q"], bf, (rows, H * D), "Q", strided=True), _want(g["O"], bf, (rows, H * D), "O", strided=True),
+                   c.codes.data_ptr(), c.scales.data_ptr(), rows, H, c.kv_heads, D, c.n_pages, _row_stride(g["Q"]), _row_stride(g["O"]),
+                   int(g.get("window") or 0), D ** -0.5 if g.get("scale") is None else float(g["scale"]), float(g.get("softcap") or 0.0), (0, 0))
+    return args
+
+
+def _attn_workspace(plan, device):
+    """A workspace whose counters are zero (None if the plan needs none), once it is: the copy that clears it is waited for by the caller."""
+    if not plan.workspace_bytes:
+        return None
+    t = torch.empty(plan.workspace_bytes, dtype=torch.uint8, device=device)
+    B.epara_workspace_init(t.data_ptr(), min(plan.workspace_bytes // 256 * 256, -(-4 * sum(plan.n_items) // 256) * 256), current_stream_handle())
+    return t
+
+
 class CacheAttnPlan:
     """Arguments of one epara_cache_attention call.  groups: per service of the table a dict with Q and O [rows, heads head_dim] (bf16; Q may be the first
     columns of a QKV projection's output), cache (PagedCache), heads, and optionally scale (1 / sqrt(head_dim)), window and softcap (0: none)."""
 
     def __init__(self, table, groups, device):
         _require_gpu()
-        if len(groups) != table.G:
-            raise ValueError("%d services in the table, %d groups" % (table.G, len(groups)))
-        self.table, self.args = table, np.zeros(len(groups), dtype=B.CACHE_ATTN_ARGS)
-        bf = torch.bfloat16
-        for i, g in enumerate(groups):
-            c, H = g["cache"], int(g["heads"])
-            rows, D = int(g["Q"].shape[0]), c.head_dim
-            self.args[i] = (_want(g["Q"], bf, (rows, H * D), "Q", strided=True), _want(g["O"], bf, (rows, H * D), "O", strided=True),
-                            c.codes.data_ptr(), c.scales.data_ptr(), rows, H, c.kv_heads, D, c.n_pages, _row_stride(g["Q"]), _row_stride(g["O"]),
-                            int(g.get("window") or 0), D ** -0.5 if g.get("scale") is None else float(g["scale"]), float(g.get("softcap") or 0.0), (0, 0))
-        self.first, self.plan = self._cut(groups, n_compute_units(device))
-        self._upload(device)
-        self.d_workspace, at = None, 0
-        if self.plan.workspace_bytes:
-            self.d_workspace = torch.empty(self.plan.workspace_bytes, dtype=torch.uint8, device=device)
-            at = self.d_workspace.data_ptr()
-            counters = 4 * (self.plan.n_items[0] + self.plan.n_items[1])
-            B.epara_workspace_init(at, -(-counters // 256) * 256, current_stream_handle())
-        self.c = B.CacheAttnLaunch(self.args.ctypes.data, self.d_args.data_ptr(), self.first.ctypes.data, self.d_first.data_ptr(), at or None,
+        self.table, self.args = table, _attn_args(table, groups)
+        self.first, self.plan = B.epara_plan_cache_attention(self.args, table.c, n_compute_units(device))
+        self.d_args, self.d_first = _upload_all([self.args, self.first], device)
+        self.d_workspace = _attn_workspace(self.plan, device)
+        at = None if self.d_workspace is None else self.d_workspace.data_ptr()
+        self.c = B.CacheAttnLaunch(self.args.ctypes.data, self.d_args.data_ptr(), self.first.ctypes.data, self.d_first.data_ptr(), at,
                                    self.plan.workspace_bytes, table.c, self.plan, len(self.args), 0)
         torch.cuda.synchronize(device)
         self._keep = groups
-        self._call = self._bind()
-
-    def _cut(self, groups, units):
-        return B.epara_plan_cache_attention(self.args, self.table.c, units)
-
-    def _upload(self, device):
-        self.d_args, self.d_first = _upload_all([self.args, self.first], device)
-
-    def _bind(self):
-        return B.Call("epara_cache_attention", ctypes.addressof(self.c))
+        self._call = B.Call("epara_cache_attention", ctypes.addressof(self.c))
 
 
 def cache_attention(plan, stream=None):
     plan._call(_stream_of_call() if stream is None else stream)
 
 
-class TreeAttnPlan(CacheAttnPlan):
+class TreeAttnPlan:
     """Arguments of one epara_tree_attention call: groups as of CacheAttnPlan, with visible (int64 [rows, 4], as epara_draft_trees writes it) where a service's sequences
     are trees."""
 
-    def _cut(self, groups, units):
-        self.trees = np.zeros(len(groups), dtype=B.TREE_ARGS)
+    def __init__(self, table, groups, device):
+        _require_gpu()
+        self.table, self.args, self.trees = table, _attn_args(table, groups), np.zeros(len(groups), dtype=B.TREE_ARGS)
         for i, g in enumerate(groups):
             rows = int(g["Q"].shape[0])
             self.trees[i] = (0, _want(g.get("visible"), torch.int64, (rows, B.EPARA_TREE_MAX_ROWS // 64), "visible", True), 0, rows, 0)
-        return B.epara_plan_tree_attention(self.args, self.trees, self.table.c, units)
-
-    def _upload(self, device):
+        self.first, self.plan = B.epara_plan_tree_attention(self.args, self.trees, table.c, n_compute_units(device))
         self.d_args, self.d_first, self.d_trees = _upload_all([self.args, self.first, self.trees], device)
-
-    def _bind(self):
-        return B.Call("epara_tree_attention", ctypes.addressof(self.c), self.trees.ctypes.data, self.d_trees.data_ptr())
+        self.d_workspace = _attn_workspace(self.plan, device)
+        self.c = B.TreeAttnLaunch(self.args.ctypes.data, self.d_args.data_ptr(), self.trees.ctypes.data, self.d_trees.data_ptr(), self.first.ctypes.data, self.d_first.data_ptr(),
+                                  None if self.d_workspace is None else self.d_workspace.data_ptr(), self.plan.workspace_bytes, table.c, self.plan, len(self.args), 0)
+        torch.cuda.synchronize(device)
+        self._keep = groups
+        self._call = B.Call("epara_tree_attention", ctypes.addressof(self.c))
 
 
 def tree_attention(plan, stream=None):

@@ -216,14 +216,16 @@ def test_trees_behind_long_contexts_are_cut_and_joined(n, D):
         assert torch.equal(c[2]["O"].view(torch.int16), first.view(torch.int16))
 
 
-def test_a_chain_has_the_bits_of_causal_attention_where_both_take_the_same_kernel():
+def test_a_chain_is_causal_attention_in_every_kernel():
+    """Both calls against the causal oracle: 12 to 400 rows to a key head, next to enough others that each of the kernels runs."""
     rng = np.random.default_rng(68)
-    c = tree_case(rng, [40, 0, 1000], [list(range(-1, n - 1)) for n in (3, 8, 5)], 8, 2, 128)
-    run_tree_attn([c])
-    O = c[2]["O"].clone()
-    R.cache_attention(R.CacheAttnPlan(R.SequenceTable([c[1]], DEV), [c[2]], DEV))
-    sync()
-    assert torch.equal(O.view(torch.int16), c[2]["O"].view(torch.int16))
+    for news in ((3, 8, 5), (20, 33, 70), (70, 90, 100), (3, 16, 100, 200)):
+        c = tree_case(rng, [40, 0, 1000, 77][: len(news)], [list(range(-1, n - 1)) for n in news], 8, 2, 128)
+        for call, plan in ((R.tree_attention, R.TreeAttnPlan), (R.cache_attention, R.CacheAttnPlan)):
+            c[2]["O"].fill_(float("nan"))
+            call(plan(R.SequenceTable([c[1]], DEV), [c[2]], DEV))
+            sync()
+            check_tree_attn([(c[0], c[1], dict(c[2], visible=None), c[3], c[4])])
 
 
 # ---- verification ------------------------------------------------------------------------------------------------
