@@ -5,7 +5,8 @@
 
 Every service has its own weights, cache and sequences; a step takes new tokens for any of them, prompts and single tokens alike, through
 ten launches.  With an fp8 FFN the second normalisation writes E4M3 codes with the service's static scale, which the gated forward reads.
-Sequences may be forked (whole pages are shared, a part-filled one is copied), released, and their pages compacted."""
+Sequences may be forked (whole pages are shared, a part-filled one is copied), released, and their pages compacted.  A step's tokens may be drafts, as a chain or a tree:
+accept() then says which of them stay, given the model's logits, and draws the next token.  Sequences that wait for it can neither step nor be forked."""
 import numpy as np
 import torch
 
@@ -42,8 +43,15 @@ class DecoderBlock:
         self.rotary = f32(np.stack([np.cos(angle), np.sin(angle)], axis=-1))
 
     # ---- sequences
+    @property
+    def drafts(self):
+        """Per service the sequences whose last step's tokens were drafts: name -> (position of the first, parents)."""
+        return self.__dict__.setdefault("_drafts", [{} for _ in self.params])
+
     def fork(self, service, name, child):
         pages, tokens = self.sequences[service][name]
+        if name in self.drafts[service]:
+            raise ValueError("sequence %r has drafts that wait to be accepted" % (name,))
         if child in self.sequences[service]:
             raise ValueError("sequence %r exists" % (child,))
         own, moves = self.pools[service].fork(pages, tokens)
@@ -56,6 +64,7 @@ class DecoderBlock:
 
     def release(self, service, name):
         self.pools[service].free(self.sequences[service].pop(name)[0])
+        self.drafts[service].pop(name, None)
 
     def compact(self, service):
         """-> how many pages moved."""
@@ -78,18 +87,82 @@ class DecoderBlock:
             R.copy_pages(R.PageCopyPlan([{"cache": self.caches[service], "moves": moves}], self.device))
 
     # ---- one step
-    def step(self, new):
+    def step(self, new, parents=None):
         """new: per service a list of (sequence name, X [tokens, d] bf16 on the GPU) -> per service a dict of the step's tensors, rows in the order of the list.  A name that
-        is not known yet begins a sequence.  A step that raises leaves all sequences and pages as they were: EparaError (ERR_CAPACITY) where a service has too few
-        free pages, ValueError for a name twice, tokens of another shape, or more positions than the table of angles has."""
+        is not known yet begins a sequence.  parents: per service a dict with a list of ints for each name whose tokens are drafts: the row (counted from the sequence's first of this
+        step) that each row follows; -1: the tokens before.  A step that raises leaves all sequences and pages as they were: EparaError (ERR_CAPACITY) where a service has too few
+        free pages, ValueError for a name twice, tokens of another shape, more positions than the table of angles has, drafts that still wait to be accepted, or parents that
+        are not as many as the tokens."""
+        trees = self._trees(new, parents)
         work = self._admit(new)
         try:
-            tensors = self._launch(new, work)
+            tensors = self._launch(new, work, trees) if any(trees) else self._launch(new, work)
         except BaseException:
             self._give_back(work)
             raise
-        self._commit(work)
+        self._commit(work, trees)
         return tensors
+
+    def _trees(self, new, parents):
+        if parents is not None and len(parents) != len(self.params):
+            raise ValueError("%d services, parents for %d" % (len(self.params), len(parents)))
+        trees = [dict(p or {}) for p in parents] if parents is not None else [{} for _ in self.params]
+        for items, own, waiting in zip(new, trees, self.drafts):
+            rows = {name: int(X.shape[0]) for name, X in items}
+            for name in rows:
+                if name in waiting:
+                    raise ValueError("sequence %r has drafts that wait to be accepted" % (name,))
+            for name, p in own.items():
+                own[name] = [int(v) for v in p]
+                if len(own[name]) != rows.get(name) or not 1 <= len(own[name]) <= B.EPARA_TREE_MAX_ROWS:
+                    raise ValueError("sequence %r: a parent for each of 1 to %d tokens of this step" % (name, B.EPARA_TREE_MAX_ROWS))
+        return trees
+
+    def accept(self, judged, temperatures):
+        """Which drafts stay, and the token behind them.  judged: per service None (no sequence waits), or a dict with the rows of its waiting sequences, one after the other as they came into
+        their steps: logits [rows, vocab] (bf16 or float32, the same for all services), tokens (int32 [rows]), uniforms (float32 [rows]) and optionally draft_logits, as of
+        runtime.VerifyPlan; temperatures: per service a list, one for each of these sequences (0: greedy).  -> per service a dict name -> (rows that stay, next token); the sequences then have
+        the tokens of those rows, the caches too, and pages that only other drafts lay in are free.  Waits for the GPU.  ValueError, and nothing changed, for rows or temperatures that do not fit."""
+        dev, kinds = self.device, {j["logits"].dtype for j in judged if j is not None}
+        kind = kinds.pop() if len(kinds) == 1 else torch.bfloat16
+        if len(judged) != len(self.params) or len(temperatures) != len(self.params):
+            raise ValueError("%d services" % len(self.params))
+        table, groups, kept = [], [], []
+        for g, (j, waiting, t) in enumerate(zip(judged, self.drafts, temperatures)):
+            rows = sum(len(p) for _, p in waiting.values())
+            if (j is None) != (not waiting) or (j is not None and int(j["logits"].shape[0]) != rows) or len(t or ()) != len(waiting):
+                raise ValueError("service %d: %d rows of %d sequences wait" % (g, rows, len(waiting)))
+            seqs, row, parents = [], 0, []
+            for name, (start, p) in waiting.items():
+                seqs.append({"first_row": row, "rows": len(p), "start": start, "pages": self.sequences[g][name][0]})
+                parents += p
+                row += len(p)
+            table.append(seqs)
+            none = lambda dtype, *shape: torch.empty(shape, dtype=dtype, device=dev)
+            j = j or {"logits": none(kind, 0, 1), "tokens": none(torch.int32, 0), "uniforms": none(torch.float32, 0)}
+            groups.append({"logits": j["logits"], "tokens": j["tokens"], "uniforms": j["uniforms"], "draft_logits": j.get("draft_logits"),
+                           "parents": torch.tensor(parents, dtype=torch.int32, device=dev)})
+            kept += list(t or ())
+        if not kept:
+            return [{} for _ in self.params]
+        seqs = R.SequenceTable(table, dev)
+        verify = R.VerifyPlan(seqs, groups, dev, temperatures=torch.tensor(kept, dtype=torch.float32, device=dev))
+        keep = R.CacheKeepPlan(seqs, [{"service": g, "cache": c, "path": own["path"]} for g, (c, own) in enumerate(zip(self.caches, verify.groups))], dev, verify.kept)
+        R.verify_drafts(verify)
+        R.cache_keep(keep)
+        counts, tokens, at, out = verify.kept.tolist(), verify.next.tolist(), 0, []
+        for g, (waiting, own) in enumerate(zip(self.drafts, verify.groups)):
+            path, row, got = own["path"].tolist(), 0, {}
+            for name, (start, p) in waiting.items():
+                n, pages = counts[at], self.sequences[g][name][0]
+                used = -(-(start + n) // B.EPARA_CACHE_PAGE)
+                self.pools[g].free(pages[used:])
+                self.sequences[g][name] = [pages[:used], start + n]
+                got[name] = (path[row: row + n], tokens[at])
+                row, at = row + len(p), at + 1
+            waiting.clear()
+            out.append(got)
+        return out
 
     def _admit(self, new):
         """-> per service a list of (name, position of the first new token, tokens, pages with the new ones, the new ones): checked, and the pages taken; no sequence is
@@ -123,12 +196,15 @@ class DecoderBlock:
             for _, _, _, _, fresh in reversed(items):
                 self.pools[g].free(fresh[::-1])
 
-    def _commit(self, work):
+    def _commit(self, work, trees=None):
         for g, items in enumerate(work):
             for name, start, n, pages, _ in items:
-                self.sequences[g][name] = [pages, start + n]
+                draft = trees is not None and name in trees[g]
+                self.sequences[g][name] = [pages, start if draft else start + n]
+                if draft:
+                    self.drafts[g][name] = (start, trees[g][name])
 
-    def _launch(self, new, work):
+    def _launch(self, new, work, trees=None):
         dev, bf = self.device, B.EPARA_BF16
         table, tensors = [], []
         for g, (items, p) in enumerate(zip(new, self.params)):
@@ -147,15 +223,29 @@ class DecoderBlock:
         R.add_rmsnorm(self._norm(tensors, "x", None, 0, None, "y1"))
         R.grouped_forward(self._forward(tensors, "qkv", "y1", "qkv"), bf)
         seqs = R.SequenceTable(table, dev)
-        R.cache_append(R.CacheAppendPlan(seqs, [{"QKV": t["qkv"], "Q": t["q"], "cache": c, "heads": p.heads, "rotary": self.rotary}
+        if trees:
+            self._follow(seqs, tensors, work, trees)
+        R.cache_append(R.CacheAppendPlan(seqs, [{"QKV": t["qkv"], "Q": t["q"], "cache": c, "heads": p.heads, "rotary": self.rotary, "positions": t.get("positions")}
                                                 for t, c, p in zip(tensors, self.caches, self.params)], dev))
-        R.cache_attention(R.CacheAttnPlan(seqs, [{"Q": t["q"], "O": t["o"], "cache": c, "heads": p.heads} for t, c, p in zip(tensors, self.caches, self.params)], dev))
+        attend, plan = (R.tree_attention, R.TreeAttnPlan) if trees else (R.cache_attention, R.CacheAttnPlan)
+        attend(plan(seqs, [{"Q": t["q"], "O": t["o"], "cache": c, "heads": p.heads, "visible": t.get("visible")} for t, c, p in zip(tensors, self.caches, self.params)], dev))
         R.grouped_forward(self._forward(tensors, "proj", "o", "proj"), bf)
         R.add_rmsnorm(self._norm(tensors, "x", "proj", 1, "s2", "y2"))
         up, down = self._ffn(tensors)
         R.grouped_ffn_swiglu(up, down, self.ffn, bf)
         R.add_rmsnorm(self._norm(tensors, "s2", "f", 0, "s3", "y3"))
         return tensors
+
+    def _follow(self, seqs, tensors, work, trees):
+        """Which rows the rows of this step follow, and their positions, next to its tensors: where tokens are no drafts each follows the one before."""
+        groups = []
+        for items, own in zip(work, trees):
+            parents = [v for name, _, n, _, _ in items for v in own.get(name, range(-1, n - 1))]
+            groups.append({"parents": torch.tensor(parents, dtype=torch.int32, device=self.device)})
+        plan = R.DraftTreePlan(seqs, groups, self.device)
+        R.draft_trees(plan)
+        for t, g in zip(tensors, plan.groups):
+            t.update(g)
 
     def _norm(self, tensors, x, r, which, s, y):
         return R.RmsNormPlan([{"X": t[x], "R": None if r is None else t[r], "gamma": gamma[which], "S": None if s is None else t[s], "Y": t[y], "eps": p.eps, "out_scale": self.s_x}
