@@ -123,10 +123,12 @@ class DecoderBlock:
         their steps: logits [rows, vocab] (bf16 or float32, the same for all services), tokens (int32 [rows]), uniforms (float32 [rows]) and optionally draft_logits, as of
         runtime.VerifyPlan; temperatures: per service a list, one for each of these sequences (0: greedy).  -> per service a dict name -> (rows that stay, next token); the sequences then have
         the tokens of those rows, the caches too, and pages that only other drafts lay in are free.  Waits for the GPU.  ValueError, and nothing changed, for rows or temperatures that do not fit."""
-        dev, kinds = self.device, {j["logits"].dtype for j in judged if j is not None}
-        kind = kinds.pop() if len(kinds) == 1 else torch.bfloat16
         if len(judged) != len(self.params) or len(temperatures) != len(self.params):
             raise ValueError("%d services" % len(self.params))
+        if any(j is not None and not {"logits", "tokens", "uniforms"} <= set(j) for j in judged):
+            raise ValueError("logits, tokens and uniforms of the rows that wait")
+        dev, kinds = self.device, {j["logits"].dtype for j in judged if j is not None}
+        kind = kinds.pop() if len(kinds) == 1 else torch.bfloat16
         table, groups, kept = [], [], []
         for g, (j, waiting, t) in enumerate(zip(judged, self.drafts, temperatures)):
             rows = sum(len(p) for _, p in waiting.values())
