@@ -93,7 +93,7 @@ struct head_pages {
 };
 
 // One block of 32 tokens: its tokens [lo, hi) come from the slots start + path[..] (all at or behind their own), those before lo are earlier ones.
-// Lane t (and t + 32) knows token t.  All is read before anything is written; nothing that a later block reads lies in this one.
+// Lane t (and t + 32) knows token t.  All keys are read before any is written, and all values; nothing that a later block reads lies in this one.
 template <int D>
 __device__ __forceinline__ void keep_block(const head_pages& c, int block, int lo, int hi, int src, int lane)
 {
@@ -118,42 +118,7 @@ __device__ __forceinline__ void keep_block(const head_pages& c, int block, int l
         const int from = __shfl(comes ? src : block * BLOCK + token, t), at = from & (PAGE - 1), in = __shfl(page, t);
         key_shift[p] = __shfl(was_k, t) - e_k;
         key[p] = v4i{0, 0, 0, 0};
-        if (t < hi) key[p] = *reinterpret_cast<const EPARA_GLOBAL v4i*>(c.keys(in) + ((((at / 4) % 4) * CD + chunk) * 16 + 4 * (at / 16) + at % 4) * 16);
-    }
-    // ---- values: a lane takes whole dims.  What the block holds, and the tokens that come, byte by byte
-    v4i value[DIMS][2];
-    EPARA_GLOBAL char* value_at[DIMS][2];
-#pragma unroll
-    for (int d = 0; d < DIMS; ++d)
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const int dim = lane + 64 * d;
-            value_at[d][q] = c.keys(home) + PAGE * D + ((dim / 16 * 4 + 2 * half + q) * 16 + dim % 16) * 16;
-            value[d][q] = *reinterpret_cast<const EPARA_GLOBAL v4i*>(value_at[d][q]);
-        }
-    const int own_shift = c.scale(home)[2 + half] - 127 - e_v;
-    if (lo > 0 && own_shift < 0) {                         // earlier tokens of a block that grows
-#pragma unroll
-        for (int d = 0; d < DIMS; ++d)
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int mask = low_bytes(lo - 16 * q - 4 * j);
-                    value[d][q][j] = (rescaled(value[d][q][j], own_shift) & mask) | (value[d][q][j] & ~mask);
-                }
-    }
-#pragma unroll
-    for (int t = 0; t < BLOCK; ++t) {
-        if (t < lo || t >= hi) continue;
-        const int from = __builtin_amdgcn_readlane(src, t), in = __builtin_amdgcn_readlane(page, t), at = from & (PAGE - 1), shift = __builtin_amdgcn_readlane(was_v, t) - e_v;
-#pragma unroll
-        for (int d = 0; d < DIMS; ++d) {
-            const int dim = lane + 64 * d;
-            const int byte = *reinterpret_cast<const EPARA_GLOBAL uint8_t*>(c.keys(in) + PAGE * D + ((dim / 16 * 4 + at / 16) * 16 + dim % 16) * 16 + at % 16);
-            const int others = value[d][t / 16][t % 16 / 4] & ~(0xff << 8 * (t % 4));
-            value[d][t / 16][t % 16 / 4] = others | (rescaled(byte, shift) & 0xff) << 8 * (t % 4);
-        }
+        if (t < hi && (t >= lo || key_shift[p] != 0)) key[p] = *reinterpret_cast<const EPARA_GLOBAL v4i*>(c.keys(in) + ((((at / 4) % 4) * CD + chunk) * 16 + 4 * (at / 16) + at % 4) * 16);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
@@ -164,11 +129,62 @@ __device__ __forceinline__ void keep_block(const head_pages& c, int block, int l
         for (int j = 0; j < 4; ++j) key[p][j] = rescaled(key[p][j], key_shift[p]);
         *reinterpret_cast<EPARA_GLOBAL v4i*>(c.keys(home) + ((((at / 4) % 4) * CD + chunk) * 16 + 4 * (at / 16) + at % 4) * 16) = key[p];
     }
+    // ---- values: a lane takes whole dims.  What the block holds, and the tokens that come, byte by byte: four at a time, whether all are wanted or not
+    const int own_shift = lo > 0 ? __builtin_amdgcn_readfirstlane(was_v) - e_v : 0;          // token 0 is an earlier one then
+    auto touched = [&](int q) { return hi > 16 * q && (lo < 16 * q + 16 || own_shift < 0); };
+    v4i value[DIMS][2];
+    EPARA_GLOBAL char* value_at[DIMS][2];
+#pragma unroll
+    for (int d = 0; d < DIMS; ++d)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int dim = lane + 64 * d;
+            value_at[d][q] = c.keys(home) + PAGE * D + ((dim / 16 * 4 + 2 * half + q) * 16 + dim % 16) * 16;
+            value[d][q] = v4i{0, 0, 0, 0};
+            if (touched(q)) value[d][q] = *reinterpret_cast<const EPARA_GLOBAL v4i*>(value_at[d][q]);
+        }
+    if (own_shift < 0) {                         // earlier tokens of a block that grows
+#pragma unroll
+        for (int d = 0; d < DIMS; ++d)
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int mask = low_bytes(lo - 16 * q - 4 * j);
+                    value[d][q][j] = (rescaled(value[d][q][j], own_shift) & mask) | (value[d][q][j] & ~mask);
+                }
+    }
+    const int slot = comes ? src : block * BLOCK + token;
+#pragma unroll
+    for (int t0 = 0; t0 < BLOCK; t0 += 4) {
+        if (t0 + 4 <= lo || t0 >= hi) continue;
+        int byte[4][DIMS];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int at = __builtin_amdgcn_readlane(slot, t0 + t) & (PAGE - 1), in = __builtin_amdgcn_readlane(page, t0 + t);
+#pragma unroll
+            for (int d = 0; d < DIMS; ++d) {
+                const int dim = lane + 64 * d;
+                byte[t][d] = *reinterpret_cast<const EPARA_GLOBAL uint8_t*>(c.keys(in) + PAGE * D + ((dim / 16 * 4 + at / 16) * 16 + dim % 16) * 16 + at % 16);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            if (t0 + t < lo || t0 + t >= hi) continue;
+            const int shift = __builtin_amdgcn_readlane(was_v, t0 + t) - e_v;
+#pragma unroll
+            for (int d = 0; d < DIMS; ++d) {
+                const int others = value[d][t0 / 16][t0 % 16 / 4] & ~(0xff << 8 * t);
+                value[d][t0 / 16][t0 % 16 / 4] = others | (rescaled(byte[t][d], shift) & 0xff) << 8 * t;
+            }
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
     for (int d = 0; d < DIMS; ++d)
 #pragma unroll
         for (int q = 0; q < 2; ++q)
-            if (hi > 16 * q && (lo < 16 * q + 16 || own_shift < 0)) *reinterpret_cast<EPARA_GLOBAL v4i*>(value_at[d][q]) = value[d][q];
+            if (touched(q)) *reinterpret_cast<EPARA_GLOBAL v4i*>(value_at[d][q]) = value[d][q];
     if (lane == 0) {
         c.scale(home)[half] = static_cast<uint8_t>(e_k + 127);
         c.scale(home)[2 + half] = static_cast<uint8_t>(e_v + 127);
@@ -176,7 +192,7 @@ __device__ __forceinline__ void keep_block(const head_pages& c, int block, int l
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
-__global__ __launch_bounds__(NT) void cache_keep_kernel(const epara_keep_args* __restrict__ caches, int n_caches, const epara_sequence* __restrict__ seqs,
+__global__ __launch_bounds__(NT, 4) void cache_keep_kernel(const epara_keep_args* __restrict__ caches, int n_caches, const epara_sequence* __restrict__ seqs,
                                                        const int32_t* __restrict__ pages, const int32_t* __restrict__ kept, int n_items)
 {
     const int lane = threadIdx.x & 63, item = blockIdx.x * (NT / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
