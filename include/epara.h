@@ -1122,8 +1122,8 @@ typedef struct {
  * (given), max(p_r - q_r, 0) if it has a child with a token of the vocabulary (drawn), or p_r.  Where all of w is 0 it is the one with the largest logit.
  * A row whose logits have a NaN, +infinity or nothing above -infinity has no distribution: no child of it stays, the next token behind it is -1, probabilities are 0; drafts' logits of
  * that kind: the child does not stay and the next token is drawn from p_r.  Uniforms below 0 and NaN count as 0, those from 1 on as the largest number below.
- * Sums and probabilities that decide about drafts are fp32 products summed in fp64; the next token's weights and sums are fp64 throughout, since the borders between tokens lie close.
- * Logits of every row are read once, draft logits of rows with a child once, and those of the row behind which a token is drawn again.
+ * A row's sum is of fp32 exponentials, in fp32 over up to 64 of them and in fp64 beyond; the next token's weights and sums are fp64 throughout, since the borders between tokens lie
+ * close.  Logits of every row are read once, draft logits of rows with a child once, and those of the row behind which a token is drawn again.  Three kernels (two without temperatures).
  * Errors: ERR_NULL; ERR_DTYPE; ERR_SHAPE (a dimension out of range, a sequence of too many rows or outside the service's, a row of two sequences, h_first not the plan's); ERR_ALIGN (pointers
  * not a multiple of their elements' size, workspace); ERR_CAPACITY (workspace, too much work for one grid, or no host memory). */
 int32_t epara_plan_verify_drafts(const epara_verify_args* h_args, int32_t G, const epara_sequence_table* table, int32_t dtype, int32_t n_compute_units,

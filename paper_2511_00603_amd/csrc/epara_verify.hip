@@ -8,6 +8,12 @@
 // know r before it sums; it knows r0 from the first, off by some 10^-7.  F(r) = sum max(a - r b, 0) is piecewise linear, so it sums F(r0) and its slope -G = -sum of b where a > r0 b
 // next to sum a and sum b, and the last workgroup has r and F(r) = F(r0) - (r - r0) G, wrong only by elements with a / b between r0 and r: (r - r0) times their share
 // of q.  Where so little is left that this could matter, the last workgroup sums all chunks once more with r.
+//
+// The first kernel is bound by HBM: chains of four drafts of 64 requests at 131072 tokens, with draft logits (0.15 GB), 31 us, 4.9 TB/s, of 65 for the whole call; the second takes 5 to 10 us, a
+// chain of dependent trips to memory, and a workgroup to a sequence; the third 31 us there (two rows of 131072 weights in 64 bits to a sequence, at 4 waves to a SIMD) and 6 to 11 elsewhere.
+// What was measured on the way: the walk by the last of the first kernel's workgroups instead of a kernel of its own 32 -> 70 us (each of 5760 short workgroups then waits for its store and
+// its counter); the walk and the draw in one kernel, walked again by every workgroup, 36 us and more; a third kernel that sums first and a fourth that draws from max(p - q, 0): 26 + 48 us;
+// loops over siblings that branch at each 14 us; scans through the LDS' shuffles and searches by atomics 5 us of the third kernel's 11 at one request.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>

@@ -200,6 +200,28 @@ def test_trees_next_to_prompts_and_services_without_trees():
     check_tree_attn(cases)
 
 
+def test_padded_sequences_of_a_service_without_trees():
+    """In front of position 0 rows see nothing and get zeros, in each kind of tile, next to a service of trees."""
+    rng = np.random.default_rng(69)
+    trees = tree_case(rng, [40, 3], [random_tree(rng, 9), random_tree(rng, 70)], 4, 2, 64)
+    case = Case(rng, [0, 9, 3, 30, 120], 4, 2, 64)
+    starts, news = [-5, -1, -30, -3, -180], [5, 10, 33, 33, 300]
+    case.fill([0, 9, 3, 30, 120])
+    seqs, rows = sequences(case, starts, news)
+    q, Q = dev_bf16(rng.standard_normal((rows, 4 * 64)))
+    O = torch.full((rows, 4 * 64), float("nan"), dtype=torch.bfloat16, device=DEV)
+    g = {"Q": Q, "O": O, "cache": case.cache, "heads": 4, "window": 0, "softcap": 0.0, "visible": None}
+    R.tree_attention(R.TreeAttnPlan(R.SequenceTable([trees[1], seqs], DEV), [trees[2], g], DEV))
+    sync()
+    check_tree_attn([trees])
+    got = fetch(O).reshape(rows, 4, 64)
+    for s, n in zip(seqs, news):
+        part = slice(s["first_row"], s["first_row"] + n)
+        K, V = case.oracle.values(s["pages"], max(s["start"] + n, 0))
+        want, mass = OD.attention(q.reshape(rows, 4, 64)[part], K, V, s["start"], 64 ** -0.5)
+        assert (np.abs(got[part] - want) <= (2.0 ** -8 + 2.0 ** -10) * mass + BF * np.abs(want)).all(), s["start"]
+
+
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("n", [4, 16, 40, 100])
 def test_trees_behind_long_contexts_are_cut_and_joined(n, D):
