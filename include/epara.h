@@ -1146,7 +1146,7 @@ typedef struct {
 /* The rows that stay move together: for each sequence, token start + path[i] of its pages becomes token start + i, for i < d_kept[its index in the table].  A block of 32 tokens
  * that gets any takes the largest of the exponents that its tokens (earlier ones too) have; codes are rescaled, and rounded again, only where that is more than they had.  What else lies
  * in the pages is left as it is.  A path that does not rise, or leaves the sequence's rows, ends there; kept is held to 0 .. rows.  Nothing moves in a sequence of more than
- * EPARA_TREE_MAX_ROWS rows.  One kernel, a wave to a cache, sequence and head.
+ * EPARA_TREE_MAX_ROWS rows.  One kernel, two waves to a cache, sequence and head.
  * Errors: ERR_NULL; ERR_SHAPE (a dimension out of range, rows outside the service's, a tree that starts before position 0, a page outside the cache or under new rows of two
  * sequences of one cache, a cache twice, first_seq or first_item not the table's); ERR_ALIGN; ERR_CAPACITY (too much work for one grid, or no host memory). */
 int32_t epara_cache_keep(const epara_keep_args* h_caches, const epara_keep_args* d_caches, int32_t n_caches, const epara_sequence_table* table,

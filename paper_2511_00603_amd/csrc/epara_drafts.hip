@@ -1,7 +1,8 @@
 // libepara: trees of drafted tokens: who follows whom, and closing up the tokens that stay in a paged cache.
 //
 // Both are bound by latency: a tree is 12 KiB at most, and what stays of one are a few tokens of each head.  Trees of 205 sequences with 33 to 256 rows 4.7 us, of one 4.1, a launch and three
-// trips to memory.  Keeping: one request in 32 layers of 8 heads 4.6 us, 40 requests in 16 layers 18.4 us: 5120 waves of some ten dependent trips each, four to a SIMD at 126 registers.
+// trips to memory.  Keeping: one request in 32 layers of 8 heads 4.6 us, 40 requests in 16 layers 15.4 us: 10240 waves, half of them for keys and half for values, of some nine dependent
+// trips each, five to a SIMD at 90 registers.  One wave for both was longer and needed 126: 18.4 us.  More waves with spilled registers: six 21.2, eight 29.0.
 // (A value is a byte of each of a head's dims, so a token that moves costs a read and a write of its 16 tokens' chunks.)
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -70,7 +71,7 @@ __global__ __launch_bounds__(NT) void draft_trees_kernel(const epara_tree_args* 
     if (positions) put_position(tid, s.start + max_of(n - 1, 0));
 }
 
-// ---- keeping: a wave per cache, sequence and head
+// ---- keeping: two waves per cache, sequence and head, for keys and for values
 
 // Codes times 2^shift (shift <= 0), rounded again; as they are where there is no shift.  A NaN's code stays (the conversions would change its sign).
 __device__ __forceinline__ int rescaled(int codes, int shift)
@@ -86,118 +87,128 @@ __device__ __forceinline__ int rescaled(int codes, int shift)
 struct head_pages {
     char* codes;
     uint8_t* scales;
-    const int32_t* pages;        // of the sequence
+    int page, first;             // lane i has page first + i of the sequence's
     int kv_heads, head;
     size_t bytes;                // of a page and head
     __device__ __forceinline__ EPARA_GLOBAL char* keys(int page) const { return (EPARA_GLOBAL char*)codes + (static_cast<size_t>(page) * kv_heads + head) * bytes; }
     __device__ __forceinline__ EPARA_GLOBAL uint8_t* scale(int page) const { return (EPARA_GLOBAL uint8_t*)scales + (static_cast<size_t>(page) * kv_heads + head) * 4; }
-    __device__ __forceinline__ int page_of(int slot) const { return ((const EPARA_GLOBAL int32_t*)pages)[slot / PAGE]; }
+    __device__ __forceinline__ int page_of(int slot) const { return __shfl(page, slot / PAGE - first); }        // (all lanes ask)
 };
 
-// One block of 32 tokens: its tokens [lo, hi) come from the slots start + path[..] (all at or behind their own), those before lo are earlier ones.
-// Lane t (and t + 32) knows token t.  All keys are read before any is written, and all values; nothing that a later block reads lies in this one.
+// A lane takes pieces of 16 dims of a token.
 template <int D>
-__device__ __forceinline__ void keep_block(const head_pages& c, int block, int lo, int hi, int src, int lane)
+__device__ __forceinline__ void keep_keys(const head_pages& c, int half, int home, int lo, int hi, int from, int page, int was, int e, int lane)
 {
-    constexpr int CD = D / 16, PASSES = BLOCK * CD / 64, DIMS = D / 64;
-    const int token = lane & 31, half = block & 1;
-    const bool comes = token >= lo && token < hi;
-    const int home = c.page_of(block * BLOCK), page = comes ? c.page_of(src) : home, from_half = comes ? src / BLOCK & 1 : half;
-    const EPARA_GLOBAL uint8_t* sc = c.scale(page);
-    const int was_k = sc[from_half] - 127, was_v = sc[2 + from_half] - 127;          // of where the token lies now
-    int e_k = token < hi ? was_k : -1000, e_v = token < hi ? was_v : -1000;
-#pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) {
-        e_k = max_of(e_k, __shfl_xor(e_k, d));
-        e_v = max_of(e_v, __shfl_xor(e_v, d));
-    }
-    // ---- keys: a lane takes pieces of 16 dims of a token
+    constexpr int CD = D / 16, PASSES = BLOCK * CD / 64;
     v4i key[PASSES];
-    int key_shift[PASSES];
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
         const int piece = p * 64 + lane, t = piece / CD, chunk = piece % CD;
-        const int from = __shfl(comes ? src : block * BLOCK + token, t), at = from & (PAGE - 1), in = __shfl(page, t);
-        key_shift[p] = __shfl(was_k, t) - e_k;
+        const int at = __shfl(from, t) & (PAGE - 1), in = __shfl(page, t);
+        const int shift = __shfl(was, t) - e;
         key[p] = v4i{0, 0, 0, 0};
-        if (t < hi && (t >= lo || key_shift[p] != 0)) key[p] = *reinterpret_cast<const EPARA_GLOBAL v4i*>(c.keys(in) + ((((at / 4) % 4) * CD + chunk) * 16 + 4 * (at / 16) + at % 4) * 16);
+        if (t < hi && (t >= lo || shift != 0)) key[p] = *reinterpret_cast<const EPARA_GLOBAL v4i*>(c.keys(in) + ((((at / 4) % 4) * CD + chunk) * 16 + 4 * (at / 16) + at % 4) * 16);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
-        const int piece = p * 64 + lane, t = piece / CD, chunk = piece % CD, at = half * BLOCK + t;
-        if (t >= hi || (t < lo && key_shift[p] == 0)) continue;
+        const int piece = p * 64 + lane, t = piece / CD, chunk = piece % CD, at = half * BLOCK + t, shift = __shfl(was, t) - e;
+        if (t >= hi || (t < lo && shift == 0)) continue;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) key[p][j] = rescaled(key[p][j], key_shift[p]);
+        for (int j = 0; j < 4; ++j) key[p][j] = rescaled(key[p][j], shift);
         *reinterpret_cast<EPARA_GLOBAL v4i*>(c.keys(home) + ((((at / 4) % 4) * CD + chunk) * 16 + 4 * (at / 16) + at % 4) * 16) = key[p];
     }
-    // ---- values: a lane takes whole dims.  What the block holds, and the tokens that come, byte by byte: four at a time, whether all are wanted or not
-    const int own_shift = lo > 0 ? __builtin_amdgcn_readfirstlane(was_v) - e_v : 0;          // token 0 is an earlier one then
-    auto touched = [&](int q) { return hi > 16 * q && (lo < 16 * q + 16 || own_shift < 0); };
-    v4i value[DIMS][2];
-    EPARA_GLOBAL char* value_at[DIMS][2];
+}
+// A lane takes whole dims, 16 tokens of them at a time (they lie together; what comes into the second 16 lies at or behind them).  What is there, and the tokens that come, byte by byte: four at a
+// time, whether all are wanted or not.
+template <int D>
+__device__ __forceinline__ void keep_values(const head_pages& c, int half, int home, int lo, int hi, int from, int page, int was, int e, unsigned lane)
+{
+    constexpr int DIMS = D / 64;
+    const int own_shift = lo > 0 ? __builtin_amdgcn_readfirstlane(was) - e : 0;          // token 0 is an earlier one then
+    const unsigned mine = lane / 16 * 1024 + lane % 16 * 16;   // of my first dim, in a page's values
+#pragma unroll 1
+    for (int q = 0; q < 2; ++q) {
+        const int lo_q = lo - 16 * q, hi_q = hi - 16 * q;
+        if (hi_q <= 0 || (lo_q >= 16 && own_shift == 0)) continue;
+        EPARA_GLOBAL char* dst = c.keys(home) + PAGE * D + (2 * half + q) * 256;
+        v4i value[DIMS];
 #pragma unroll
-    for (int d = 0; d < DIMS; ++d)
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const int dim = lane + 64 * d;
-            value_at[d][q] = c.keys(home) + PAGE * D + ((dim / 16 * 4 + 2 * half + q) * 16 + dim % 16) * 16;
-            value[d][q] = v4i{0, 0, 0, 0};
-            if (touched(q)) value[d][q] = *reinterpret_cast<const EPARA_GLOBAL v4i*>(value_at[d][q]);
-        }
-    if (own_shift < 0) {                         // earlier tokens of a block that grows
-#pragma unroll
-        for (int d = 0; d < DIMS; ++d)
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
+        for (int d = 0; d < DIMS; ++d) {
+            value[d] = *reinterpret_cast<const EPARA_GLOBAL v4i*>(dst + mine + 4096u * d);
+            if (own_shift < 0)                             // earlier tokens of a block that grows
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int mask = low_bytes(lo - 16 * q - 4 * j);
-                    value[d][q][j] = (rescaled(value[d][q][j], own_shift) & mask) | (value[d][q][j] & ~mask);
+                    const int mask = low_bytes(lo_q - 4 * j);
+                    value[d][j] = (rescaled(value[d][j], own_shift) & mask) | (value[d][j] & ~mask);
                 }
-    }
-    const int slot = comes ? src : block * BLOCK + token;
-#pragma unroll
-    for (int t0 = 0; t0 < BLOCK; t0 += 4) {
-        if (t0 + 4 <= lo || t0 >= hi) continue;
-        int byte[4][DIMS];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int at = __builtin_amdgcn_readlane(slot, t0 + t) & (PAGE - 1), in = __builtin_amdgcn_readlane(page, t0 + t);
-#pragma unroll
-            for (int d = 0; d < DIMS; ++d) {
-                const int dim = lane + 64 * d;
-                byte[t][d] = *reinterpret_cast<const EPARA_GLOBAL uint8_t*>(c.keys(in) + PAGE * D + ((dim / 16 * 4 + at / 16) * 16 + dim % 16) * 16 + at % 16);
-            }
         }
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            if (t0 + t < lo || t0 + t >= hi) continue;
-            const int shift = __builtin_amdgcn_readlane(was_v, t0 + t) - e_v;
+        for (int t0 = 0; t0 < 16; t0 += 4) {
+            if (t0 + 4 <= lo_q || t0 >= hi_q) continue;
+            int byte[4][DIMS];
 #pragma unroll
-            for (int d = 0; d < DIMS; ++d) {
-                const int others = value[d][t0 / 16][t0 % 16 / 4] & ~(0xff << 8 * t);
-                value[d][t0 / 16][t0 % 16 / 4] = others | (rescaled(byte[t][d], shift) & 0xff) << 8 * t;
+            for (int t = 0; t < 4; ++t) {
+                const int at = __builtin_amdgcn_readlane(from, 16 * q + t0 + t) & (PAGE - 1), in = __builtin_amdgcn_readlane(page, 16 * q + t0 + t);
+                const EPARA_GLOBAL uint8_t* src = reinterpret_cast<const EPARA_GLOBAL uint8_t*>(c.keys(in) + PAGE * D + at / 16 * 256 + at % 16);
+#pragma unroll
+                for (int d = 0; d < DIMS; ++d) byte[t][d] = src[mine + 4096u * d];
+            }
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                if (t0 + t < lo_q || t0 + t >= hi_q) continue;
+                const int shift = __builtin_amdgcn_readlane(was, 16 * q + t0 + t) - e;
+#pragma unroll
+                for (int d = 0; d < DIMS; ++d) value[d][t0 / 4] = (value[d][t0 / 4] & ~(0xff << 8 * t)) | (rescaled(byte[t][d], shift) & 0xff) << 8 * t;
             }
         }
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-    for (int d = 0; d < DIMS; ++d)
-#pragma unroll
-        for (int q = 0; q < 2; ++q)
-            if (touched(q)) *reinterpret_cast<EPARA_GLOBAL v4i*>(value_at[d][q]) = value[d][q];
-    if (lane == 0) {
-        c.scale(home)[half] = static_cast<uint8_t>(e_k + 127);
-        c.scale(home)[2 + half] = static_cast<uint8_t>(e_v + 127);
+        for (int d = 0; d < DIMS; ++d) *reinterpret_cast<EPARA_GLOBAL v4i*>(dst + mine + 4096u * d) = value[d];
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
-__global__ __launch_bounds__(NT, 4) void cache_keep_kernel(const epara_keep_args* __restrict__ caches, int n_caches, const epara_sequence* __restrict__ seqs,
+// One block of 32 tokens: its tokens [lo, hi) come from the slots start + path[..] (all at or behind their own), those before lo are earlier ones.
+// Lane t (and t + 32) knows token t.  All keys (values) are read before any is written; nothing that a later block reads lies in this one.
+template <int D, bool KEYS>
+__device__ __forceinline__ void keep_block(const head_pages& c, int block, int lo, int hi, int src, int lane)
+{
+    const int token = lane & 31, half = block & 1;
+    const int from = token >= lo && token < hi ? src : block * BLOCK + token;       // the slot
+    const int home = __builtin_amdgcn_readfirstlane(c.page_of(block * BLOCK)), page = c.page_of(from);
+    constexpr int SCALE = KEYS ? 0 : 2;                    // of a page's scales
+    const int was = c.scale(page)[SCALE + (from / BLOCK & 1)] - 127;        // of where the token lies now
+    int e = token < hi ? was : -1000;
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) e = max_of(e, __shfl_xor(e, d));
+    if constexpr (KEYS) keep_keys<D>(c, half, home, lo, hi, from, page, was, e, lane);
+    else                keep_values<D>(c, half, home, lo, hi, from, page, was, e, lane);
+    if (lane == 0) c.scale(home)[SCALE + half] = static_cast<uint8_t>(e + 127);
+}
+
+// Path rows still .. count - 1.
+template <int D, bool KEYS>
+__device__ __forceinline__ void keep_blocks(const head_pages& c, const epara_sequence& s, int still, int count, const int (&row)[TREE_WORDS], int lane)
+{
+#pragma unroll 1
+    for (int block = (s.start + still) / BLOCK; block <= (s.start + count - 1) / BLOCK; ++block) {
+        const int first = block * BLOCK, lo = max_of(s.start - first, 0), hi = min_of(s.start + count - first, BLOCK);
+        const int at = first + (lane & 31) - s.start;      // my token's place in the path
+        int src = 0;
+#pragma unroll
+        for (int w = 0; w < TREE_WORDS; ++w) {
+            const int r = __shfl(row[w], at & 63);
+            if (at >> 6 == w) src = s.start + r;
+        }
+        keep_block<D, KEYS>(c, block, lo, hi, src, lane);
+    }
+}
+
+__global__ __launch_bounds__(NT, 5) void cache_keep_kernel(const epara_keep_args* __restrict__ caches, int n_caches, const epara_sequence* __restrict__ seqs,
                                                        const int32_t* __restrict__ pages, const int32_t* __restrict__ kept, int n_items)
 {
-    const int lane = threadIdx.x & 63, item = blockIdx.x * (NT / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int item = blockIdx.x * (NT / 128) + (wave >> 1);
     if (item >= n_items) return;
     int g = 0, n = n_caches;                               // the last cache whose first_item is <= item
     while (n > 1) {
@@ -208,20 +219,22 @@ __global__ __launch_bounds__(NT, 4) void cache_keep_kernel(const epara_keep_args
         n = n - before < step ? n - before : step;
     }
     const epara_keep_args a = caches[__builtin_amdgcn_readfirstlane(g)];
-    const int local = item - a.first_item, i = a.first_seq + local / a.kv_heads;
+    const int local = item - a.first_item, nth = __builtin_amdgcn_readfirstlane(local / a.kv_heads), i = a.first_seq + nth;
     const epara_sequence s = seqs[i];
-    if (s.rows > TREE_ROWS) return;
-    // ---- the path: four rows of it to a lane's word, 64 rows to a word
+    if (s.rows == 0 || s.rows > TREE_ROWS) return;
+    // ---- the pages from token `start` on: no more than a wave has lanes.  And the path, 64 rows to a word
+    const int first_page = s.start / PAGE, page = ((const EPARA_GLOBAL int32_t*)pages)[static_cast<size_t>(s.first_page) + min_of(first_page + lane, s.n_pages - 1)];
     int row[TREE_WORDS], last = -1, count = max_of(0, min_of(kept[i], s.rows)), still = 0;       // still: rows at the path's beginning that stay where they are
     bool rising = true, same = true;
 #pragma unroll
     for (int w = 0; w < TREE_WORDS; ++w) {
         const int at = 64 * w + lane;
-        row[w] = at < count ? ((const EPARA_GLOBAL int32_t*)a.path)[static_cast<size_t>(s.first_row) + at] : -1;
+        row[w] = at < s.rows ? ((const EPARA_GLOBAL int32_t*)a.path)[static_cast<size_t>(s.first_row) + at] : -1;      // (before `kept` has come)
     }
     int good = 0;
 #pragma unroll
     for (int w = 0; w < TREE_WORDS; ++w) {
+        if (64 * w + lane >= count) row[w] = -1;
         int before = __shfl_up(row[w], 1);
         if (lane == 0) before = last;
         last = __builtin_amdgcn_readlane(row[w], 63);
@@ -235,19 +248,9 @@ __global__ __launch_bounds__(NT, 4) void cache_keep_kernel(const epara_keep_args
     }
     count = good;
     if (still >= count) return;
-    const head_pages c = {static_cast<char*>(a.codes), a.scales, pages + s.first_page, a.kv_heads, local - local / a.kv_heads * a.kv_heads, static_cast<size_t>(head_bytes(a.head_dim))};
-    for (int block = (s.start + still) / BLOCK; block <= (s.start + count - 1) / BLOCK; ++block) {
-        const int first = block * BLOCK, lo = max_of(s.start - first, 0), hi = min_of(s.start + count - first, BLOCK);
-        const int at = first + (lane & 31) - s.start;      // my token's place in the path
-        int src = 0;
-#pragma unroll
-        for (int w = 0; w < TREE_WORDS; ++w) {
-            const int r = __shfl(row[w], at & 63);
-            if (at >> 6 == w) src = s.start + r;
-        }
-        if (a.head_dim == 128) keep_block<128>(c, block, lo, hi, src, lane);
-        else                   keep_block<64>(c, block, lo, hi, src, lane);
-    }
+    const head_pages c = {static_cast<char*>(a.codes), a.scales, page, first_page, a.kv_heads, local - nth * a.kv_heads, static_cast<size_t>(head_bytes(a.head_dim))};
+    if (a.head_dim == 128) wave & 1 ? keep_blocks<128, false>(c, s, still, count, row, lane) : keep_blocks<128, true>(c, s, still, count, row, lane);
+    else                   wave & 1 ? keep_blocks<64, false>(c, s, still, count, row, lane) : keep_blocks<64, true>(c, s, still, count, row, lane);
 }
 
 }  // namespace
@@ -271,7 +274,7 @@ int32_t epara_cache_keep(const epara_keep_args* h_caches, const epara_keep_args*
     if (n_items == 0) return EPARA_OK;
     if (!d_caches || !d_kept) return EPARA_ERR_NULL;
     if (reinterpret_cast<uintptr_t>(d_kept) & 3) return EPARA_ERR_ALIGN;
-    hipLaunchKernelGGL(cache_keep_kernel, dim3(static_cast<unsigned>((n_items + NT / 64 - 1) / (NT / 64))), dim3(NT), 0, static_cast<hipStream_t>(stream),
+    hipLaunchKernelGGL(cache_keep_kernel, dim3(static_cast<unsigned>((n_items + NT / 128 - 1) / (NT / 128))), dim3(NT), 0, static_cast<hipStream_t>(stream),
                        d_caches, n_caches, table->d_seqs, table->d_pages, d_kept, n_items);
     return hipGetLastError() == hipSuccess ? EPARA_OK : EPARA_ERR_HIP;
 }
