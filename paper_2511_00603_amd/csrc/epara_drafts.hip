@@ -2,7 +2,8 @@
 //
 // Both are bound by latency: a tree is 12 KiB at most, and what stays of one are a few tokens of each head.  Trees of 205 sequences with 33 to 256 rows 4.7 us, of one 4.1, a launch and three
 // trips to memory.  Keeping: one request in 32 layers of 8 heads 4.6 us, 40 requests in 16 layers 15.4 us: 10240 waves, half of them for keys and half for values, of some nine dependent
-// trips each, five to a SIMD at 90 registers.  One wave for both was longer and needed 126: 18.4 us.  More waves with spilled registers: six 21.2, eight 29.0.
+// trips each, five to a SIMD at 90 registers.  One wave for both was longer and needed 126: 18.4 us.  A form of 106 registers, spilled for more waves: five 16.4, six 21.2,
+// eight 29.0.
 // (A value is a byte of each of a head's dims, so a token that moves costs a read and a write of its 16 tokens' chunks.)
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -169,7 +170,7 @@ __device__ __forceinline__ void keep_values(const head_pages& c, int half, int h
 }
 
 // One block of 32 tokens: its tokens [lo, hi) come from the slots start + path[..] (all at or behind their own), those before lo are earlier ones.
-// Lane t (and t + 32) knows token t.  All keys (values) are read before any is written; nothing that a later block reads lies in this one.
+// Lane t (and t + 32) knows token t.  All keys (of values: 16 tokens') are read before any is written; nothing that a later block reads lies in this one.
 template <int D, bool KEYS>
 __device__ __forceinline__ void keep_block(const head_pages& c, int block, int lo, int hi, int src, int lane)
 {
