@@ -5,9 +5,10 @@
 // again in 64 bits, a chunk to a workgroup; the last of them finds the chunk and in it the token.
 //
 // Where the token comes from max(p - q, 0), with weights a and b of p and q relative to their largest, that is max(a - r b, 0) with r = sum a / sum b.  The third kernel would have to
-// know r before it sums; it knows r0 from the first, off by some 10^-7.  F(r) = sum max(a - r b, 0) is piecewise linear, so it sums F(r0) and its slope -G = -sum of b where a > r0 b
+// know r before it sums; it knows r0 from the first, off by some 10^-6.  F(r) = sum max(a - r b, 0) is piecewise linear, so it sums F(r0) and its slope -G = -sum of b where a > r0 b
 // next to sum a and sum b, and the last workgroup has r and F(r) = F(r0) - (r - r0) G, wrong only by elements with a / b between r0 and r: (r - r0) times their share
-// of q.  Where so little is left that this could matter, the last workgroup sums all chunks once more with r.
+// of q.  Where so little is left that this could matter, the last workgroup sums all chunks once more with r.  Where a and r b agree over a whole chunk, both corrections leave rounding: a weight
+// under 2^-44 of a, and a chunk under 2^-42 of its a's, count as nothing, or a uniform of 0 would fall on a chunk without a token.
 //
 // The first kernel is bound by HBM: chains of four drafts of 64 requests at 131072 tokens, with draft logits (0.15 GB), 31 us, 4.9 TB/s, of 65 for the whole call; the second takes 5 to 10 us, a
 // chain of dependent trips to memory, and a workgroup to a sequence; the third 31 us there (two rows of 131072 weights in 64 bits to a sequence, at 4 waves to a SIMD) and 6 to 11 elsewhere.
@@ -32,6 +33,7 @@ constexpr int NT = 256, WAVES = NT / 64;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr double LOG2E_64 = 1.4426950408889634;
 constexpr float BELOW_ONE = 0x1.fffffep-1f;
+constexpr double SAME = 0x1p-44;             // of a weight a: a - r b under that is the rounding of r and of the sums behind it (2^-47 at most), and nothing
 
 // Where the parts of a call's workspace are.
 struct workspace {
@@ -525,6 +527,7 @@ __global__ __launch_bounds__(NT) void draw_kernel(const drawn_row* __restrict__ 
     const float u = d.uniform;
     chunk_sum* sums = all_sums + static_cast<size_t>(i) * most_chunks;
     double ratio = d.ratio, total = 0., goal = 0., base = 0.;
+    bool exact = false;                                    // the chunks' sums are of the very weights that pass 2 looks at
     // 0: my chunk's sums; 1: all chunks' once more, one after the other (only where next to nothing is left); 2: the chunk with the token
     for (int pass = 0;;) {
         float x[N];
@@ -549,10 +552,11 @@ __global__ __launch_bounds__(NT) void draw_kernel(const drawn_row* __restrict__ 
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 const double b = exp2_64((static_cast<double>(x[j]) - top_q) * unit), left = out[j] - ratio * b;
-                out[j] = fmax(left, 0.);
+                const bool some_left = left > out[j] * SAME;
+                out[j] = some_left ? left : 0.;
                 sums_of[0] += out[j];
                 sums_of[2] += b;
-                sums_of[3] += left > 0. ? b : 0.;
+                sums_of[3] += some_left ? b : 0.;
             }
         }
         const double mine = sums_of[0];
@@ -572,6 +576,7 @@ __global__ __launch_bounds__(NT) void draw_kernel(const drawn_row* __restrict__ 
             __syncthreads();
             if (!lds.last) return;
             if (pass == 1 && ++chunk < chunks) continue;
+            exact = pass == 1;
             // ---- the chunk: a thread has some of them in a row
             const int share = (chunks + NT - 1) / NT, lo = min_of(tid * share, chunks), hi = min_of(lo + share, chunks);
             double move = 0., some[1] = {0.};              // of the ratio, from what the sums were made with
@@ -586,7 +591,13 @@ __global__ __launch_bounds__(NT) void draw_kernel(const drawn_row* __restrict__ 
                 move = total / both[1] - ratio;
                 ratio += move;
             }
-            auto chunk_share = [&](int c) { return move == 0. ? get_double(&sums[c].rest) : fmax(get_double(&sums[c].rest) - move * get_double(&sums[c].q_of_rest), 0.); };
+            // (a corrected sum is no more than the chunk's own sum with r; from 4 SAME of its weights on, some of them are over SAME themselves, and it has a token)
+            auto chunk_share = [&](int c) {
+                const double all = get_double(&sums[c].rest);
+                if (move == 0.) return all;
+                const double left = all - move * get_double(&sums[c].q_of_rest);
+                return left > get_double(&sums[c].p) * (4. * SAME) ? left : 0.;
+            };
             for (int c = lo; c < hi; ++c) some[0] += chunk_share(c);
             const double share_of_mine = some[0];
             block_sums<1>(some, lds, before);
@@ -619,7 +630,14 @@ __global__ __launch_bounds__(NT) void draw_kernel(const drawn_row* __restrict__ 
             continue;
         }
         // ---- and the token in it
-        if (tid != block_find(base + before, mine, goal, lds)) return;
+        const int found = block_find(base + before, mine, goal, lds);
+        if (found < 0) {                                   // (all threads; no call leaves without a token, whatever the sums were)
+            if (exact) break;
+            pass = 1;
+            chunk = 0;
+            continue;
+        }
+        if (tid != found) return;
         int place = 0;
         double upto = base + before;
         bool done = false;
