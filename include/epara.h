@@ -1027,7 +1027,7 @@ int32_t epara_copy_pages(const epara_page_copy* h_caches, const epara_page_copy*
 
 /* One service's drafts.  Rows are those of its tensors; a parent names a row counted from its sequence's first.  -1: the row follows the tokens
  * before the call.  A row whose parent is anything but -1 or an earlier row is not there, and neither is a row that follows it: it sees nothing, nothing sees
- * it, it never stays (so that a captured step can take trees of different sizes).  A sequence of more than EPARA_TREE_MAX_ROWS rows is no tree:
+ * it, it never stays (so that a captured step can take trees of different sizes, and none of a sequence whose first row is not there).  A sequence of more than EPARA_TREE_MAX_ROWS rows is no tree:
  * its parents are not read, and each of its rows follows the one before.  32 bytes, the same on host and device. */
 typedef struct {
     const int32_t* parents;     /* device, int32 [rows] (epara_draft_trees alone reads them) */
@@ -1102,7 +1102,7 @@ typedef struct {
     const int32_t* h_first;       /* int32[n_seqs + 1] */
     const int32_t* d_first;
     const float* d_temperatures;  /* device, fp32 [n_seqs]; NULL: all 0 */
-    int32_t*     d_kept;          /* device, int32 [n_seqs], out: rows that stay, the first among them; 0 for a sequence without rows */
+    int32_t*     d_kept;          /* device, int32 [n_seqs], out: rows that stay, the first among them; 0 for a sequence without rows, or whose first row is not there */
     int32_t*     d_next;          /* device, int32 [n_seqs], out: the token behind the last of them; -1 without one */
     void*        d_workspace;     /* 256-byte aligned; one call at a time.  Its first 4 * n_seqs bytes are zeroed (epara_workspace_init) before the first call of a plan, and again
                                      after calls of another plan have used it; its own calls leave them at zero */
@@ -1114,7 +1114,8 @@ typedef struct {
 
 /* Which drafts stay, and the token behind them, so that tokens come out as if the target had drawn each of them itself (speculative sampling: Leviathan et al. 2023,
  * Chen et al. 2023; trees of given tokens: each is tried against what its elder siblings have left).  p_r = softmax(logits_r / T) with the sequence's
- * temperature T (held to [2^-100, 2^100]); T <= 0 (or a NaN): p_r is 1 at the largest logit (the lowest of equal ones).  A sequence's first row stays.  From the row r that stays last:
+ * temperature T (held to [2^-100, 2^100]); T <= 0 (or a NaN): p_r is 1 at the largest logit (the lowest of equal ones).  A sequence's first row stays, if it is there
+ * (otherwise nothing does: kept 0, a path of -1, and -1 for the next token).  From the row r that stays last:
  *   tokens are given:  its children in order, with M = 1 at first: a child c whose token x is a token of the vocabulary that no elder sibling has stays if u_c M < p_r(x);
  *                      otherwise M loses p_r(x) and the next child is tried;
  *   tokens are drawn:  its first child c alone: it stays if u_c q_r(x) < p_r(x), with q_r = softmax(draft_logits_r / T).  (With T <= 0 as above.)

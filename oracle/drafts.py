@@ -79,7 +79,7 @@ def verify(logits, draft, tokens, parents, uniforms, t):
         for c in children[r]:
             if P[r] is not None and 0 <= tokens[c] < V:
                 probs[c] = P[r][tokens[c]]
-    if n == 0:
+    if n == 0 or parents[0] != -1:                               # a first row that is not there: no row is that could stay
         return [], -1, probs, margin
     r, path = 0, [0]
     while True:

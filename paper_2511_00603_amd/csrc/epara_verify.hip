@@ -228,7 +228,7 @@ __global__ __launch_bounds__(NT) void walk_kernel(const epara_verify_args* __res
     }
     const epara_verify_args a = args[s.service];
     const int chunks = chunks_of_row(a.vocab, SIZE == 4 ? EPARA_F32 : EPARA_BF16, pieces);
-    const bool drawn = a.draft_logits != nullptr;
+    const bool drawn = a.draft_logits != nullptr, there = !a.parents || ((const EPARA_GLOBAL int32_t*)a.parents)[s.first_row] == -1;        // the first row, without which no row is
     // ---- rows: a thread knows one
     int parent = -1, token = -1;
     float uniform = 0.f;
@@ -324,14 +324,14 @@ __global__ __launch_bounds__(NT) void walk_kernel(const epara_verify_args* __res
     __syncthreads();
     if (tid == 0) {
         int n = 0;
-        for (int row = 0; row < s.rows; row = lds.child[row]) lds.path[n++] = row;
+        for (int row = there ? 0 : s.rows; row < s.rows; row = lds.child[row]) lds.path[n++] = row;
         lds.kept = n;
         lds.eldest = INT32_MAX;
         lds.n_without = 0;
     }
     __syncthreads();
     // ---- out
-    const int n = lds.kept, last = lds.path[n - 1];
+    const int n = lds.kept, last = n > 0 ? lds.path[n - 1] : 0;
     if (tid < s.rows) {
         ((EPARA_GLOBAL int32_t*)a.path)[static_cast<size_t>(s.first_row) + tid] = tid < n ? lds.path[tid] : -1;
         if (parent == last) {
@@ -341,7 +341,7 @@ __global__ __launch_bounds__(NT) void walk_kernel(const epara_verify_args* __res
     }
     __syncthreads();
     if (tid > 0) return;
-    const bool good = has_distribution(lds.sum[0][last]);
+    const bool good = n > 0 && has_distribution(lds.sum[0][last]);
     const bool rest = drawn && !temp.greedy && lds.eldest < s.rows && lds.token[lds.eldest] >= 0 && has_distribution(lds.sum[1][last]);
     kept[i] = n;
     if (!good || temp.greedy) next[i] = good ? lds.place[last] : -1;

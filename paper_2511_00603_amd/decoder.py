@@ -121,7 +121,7 @@ class DecoderBlock:
     def accept(self, judged, temperatures):
         """Which drafts stay, and the token behind them.  judged: per service None (no sequence waits), or a dict with the rows of its waiting sequences, one after the other as they came into
         their steps: logits [rows, vocab] (bf16 or float32, the same for all services), tokens (int32 [rows]), uniforms (float32 [rows]) and optionally draft_logits, as of
-        runtime.VerifyPlan; temperatures: per service a list, one for each of these sequences (0: greedy).  -> per service a dict name -> (rows that stay, next token); the sequences then have
+        runtime.VerifyPlan; temperatures: per service a list, one for each of these sequences (0: greedy).  -> per service a dict name -> (rows that stay, next token; none and -1 where the first row's parent is not -1); the sequences then have
         the tokens of those rows, the caches too, and pages that only other drafts lay in are free.  Waits for the GPU.  ValueError, and nothing changed, for rows or temperatures that do not fit."""
         if len(judged) != len(self.params) or len(temperatures) != len(self.params):
             raise ValueError("%d services" % len(self.params))
