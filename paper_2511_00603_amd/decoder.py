@@ -108,7 +108,7 @@ class DecoderBlock:
             raise ValueError("%d services, parents for %d" % (len(self.params), len(parents)))
         trees = [dict(p or {}) for p in parents] if parents is not None else [{} for _ in self.params]
         for items, own, waiting in zip(new, trees, self.drafts):
-            rows = {name: int(X.shape[0]) for name, X in items}
+            rows = {name: int(X.shape[0]) if X.dim() else 0 for name, X in items}
             for name in rows:
                 if name in waiting:
                     raise ValueError("sequence %r has drafts that wait to be accepted" % (name,))
