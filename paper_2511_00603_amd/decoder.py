@@ -132,7 +132,7 @@ class DecoderBlock:
         table, groups, kept = [], [], []
         for g, (j, waiting, t) in enumerate(zip(judged, self.drafts, temperatures)):
             rows = sum(len(p) for _, p in waiting.values())
-            if (j is None) != (not waiting) or (j is not None and int(j["logits"].shape[0]) != rows) or len(t or ()) != len(waiting):
+            if (j is None) != (not waiting) or (j is not None and (j["logits"].dim() != 2 or int(j["logits"].shape[0]) != rows)) or len(t or ()) != len(waiting):
                 raise ValueError("service %d: %d rows of %d sequences wait" % (g, rows, len(waiting)))
             seqs, row, parents = [], 0, []
             for name, (start, p) in waiting.items():

@@ -15,3 +15,13 @@ def test_tokens_of_another_shape_are_refused_as_such(tokens):
     with pytest.raises(ValueError):
         b.step([[("a", tokens)], []], [{"a": [-1]}, None])
     assert b.sequences[0]["a"][1] == 60 and not any(b.drafts)
+
+
+@pytest.mark.parametrize("logits", [torch.zeros(()), torch.zeros(2), torch.zeros(2, 3, 1)])
+def test_logits_of_another_shape_are_refused_as_such(logits):
+    b = block()
+    b.device = "cpu"
+    b._commit(b._admit([[("a", X(2))], []]), b._trees([[("a", X(2))], []], [{"a": [-1, 0]}, None]))
+    with pytest.raises(ValueError, match="service 0"):
+        b.accept([{"logits": logits, "tokens": torch.zeros(2, dtype=torch.int32), "uniforms": torch.zeros(2)}, None], [[1.0], []])
+    assert b.drafts[0] == {"a": (0, [-1, 0])}
