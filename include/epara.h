@@ -1120,7 +1120,7 @@ typedef struct {
  *                      otherwise M loses p_r(x) and the next child is tried;
  *   tokens are drawn:  its first child c alone: it stays if u_c q_r(x) < p_r(x), with q_r = softmax(draft_logits_r / T).  (With T <= 0 as above.)
  * Behind the last one that stays, the next token is the first v with sum_{i <= v} w_i > u sum_i w_i, where w is p_r without the tokens of its children
- * (given), max(p_r - q_r, 0) if it has a child with a token of the vocabulary (drawn; a difference under 2^-44 of p_r is rounding and counts as 0), or p_r.  Where all of w is 0 it is the
+ * (given), max(p_r - q_r, 0) if it has a child with a token of the vocabulary (drawn; q_r counts 2^-44 more here, so that rounding leaves nothing where both agree), or p_r.  Where all of w is 0 it is the
  * one with the largest logit.
  * A row whose logits have a NaN, +infinity or nothing above -infinity has no distribution: no child of it stays, the next token behind it is -1, probabilities are 0; drafts' logits of
  * that kind: the child does not stay and the next token is drawn from p_r.  Uniforms below 0 and NaN count as 0, those from 1 on as the largest number below.

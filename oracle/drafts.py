@@ -7,7 +7,7 @@ import numpy as np
 from . import decoder
 
 MOST = 256
-SAME = 2.0 ** -44                     # of a weight: what is left under that is rounding, and nothing
+MORE = 1 + 2.0 ** -44                 # of q: rounding leaves nothing of p - q where they agree
 
 
 def follows(parents):
@@ -117,7 +117,7 @@ def verify(logits, draft, tokens, parents, uniforms, t):
     if draft is None:
         w[[x for x in (tokens[c] for c in children[r]) if 0 <= x < V]] = 0.0
     elif children[r] and 0 <= tokens[children[r][0]] < V and q is not None:
-        w = np.where(p - q > p * SAME, p - q, 0.0)
+        w = np.maximum(p - q * MORE, 0.0)
     if not w.sum() > 0:
         return path, int(np.argmax(logits[r])), probs, margin
     cum = np.cumsum(w)

@@ -7,8 +7,8 @@
 // Where the token comes from max(p - q, 0), with weights a and b of p and q relative to their largest, that is max(a - r b, 0) with r = sum a / sum b.  The third kernel would have to
 // know r before it sums; it knows r0 from the first, off by some 10^-6.  F(r) = sum max(a - r b, 0) is piecewise linear, so it sums F(r0) and its slope -G = -sum of b where a > r0 b
 // next to sum a and sum b, and the last workgroup has r and F(r) = F(r0) - (r - r0) G, wrong only by elements with a / b between r0 and r: (r - r0) times their share
-// of q.  Where so little is left that this could matter, the last workgroup sums all chunks once more with r.  Where a and r b agree over a whole chunk, both corrections leave rounding: a weight
-// under 2^-44 of a, and a chunk under 2^-42 of its a's, count as nothing, or a uniform of 0 would fall on a chunk without a token.
+// of q.  Where so little is left that this could matter, the last workgroup sums all chunks once more with r.  Where a and r b agree over a whole chunk, F and its
+// correction cancel to their rounding, and a uniform of 0 could fall on a chunk without a token: r is taken 2^-44 larger than it is, which leaves nothing there.
 //
 // The first kernel is bound by HBM: chains of four drafts of 64 requests at 131072 tokens, with draft logits (0.15 GB), 31 us, 4.9 TB/s, of 65 for the whole call; the second takes 5 to 10 us, a
 // chain of dependent trips to memory, and a workgroup to a sequence; the third 31 us there (two rows of 131072 weights in 64 bits to a sequence, at 4 waves to a SIMD) and 6 to 11 elsewhere.
@@ -33,7 +33,7 @@ constexpr int NT = 256, WAVES = NT / 64;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr double LOG2E_64 = 1.4426950408889634;
 constexpr float BELOW_ONE = 0x1.fffffep-1f;
-constexpr double SAME = 0x1p-44;             // of a weight a: a - r b under that is the rounding of r and of the sums behind it (2^-47 at most), and nothing
+constexpr double MORE = 1. + 0x1p-44;        // of r: over the rounding of r and of the sums behind it (2^-47 at most), so that nothing is left where a = r b
 
 // Where the parts of a call's workspace are.
 struct workspace {
@@ -134,10 +134,14 @@ __device__ __forceinline__ temperature temperature_of(const float* temperatures,
     return {false, fminf(fmaxf(t, 0x1p-100f), 0x1p100f)};
 }
 
-// The row that row `row` of a sequence follows, or -1.
+// What is said to be the parent of row `row` of a sequence; the row that it follows, or -1.
+__device__ __forceinline__ int parent_word(const epara_verify_args& a, const epara_sequence& s, int row)
+{
+    return a.parents ? ((const EPARA_GLOBAL int32_t*)a.parents)[static_cast<size_t>(s.first_row) + row] : row - 1;
+}
 __device__ __forceinline__ int parent_of(const epara_verify_args& a, const epara_sequence& s, int row)
 {
-    const int p = a.parents ? ((const EPARA_GLOBAL int32_t*)a.parents)[static_cast<size_t>(s.first_row) + row] : row - 1;
+    const int p = parent_word(a, s, row);
     return p >= 0 && p < row ? p : -1;
 }
 
@@ -228,12 +232,13 @@ __global__ __launch_bounds__(NT) void walk_kernel(const epara_verify_args* __res
     }
     const epara_verify_args a = args[s.service];
     const int chunks = chunks_of_row(a.vocab, SIZE == 4 ? EPARA_F32 : EPARA_BF16, pieces);
-    const bool drawn = a.draft_logits != nullptr, there = !a.parents || ((const EPARA_GLOBAL int32_t*)a.parents)[s.first_row] == -1;        // the first row, without which no row is
+    const bool drawn = a.draft_logits != nullptr;
     // ---- rows: a thread knows one
-    int parent = -1, token = -1;
+    int up = -1, parent = -1, token = -1;
     float uniform = 0.f;
     if (tid < s.rows) {
-        parent = parent_of(a, s, tid);
+        up = parent_word(a, s, tid);
+        parent = up >= 0 && up < tid ? up : -1;
         token = ((const EPARA_GLOBAL int32_t*)a.tokens)[static_cast<size_t>(s.first_row) + tid];
         uniform = ((const EPARA_GLOBAL float*)a.uniforms)[static_cast<size_t>(s.first_row) + tid];
     }
@@ -324,7 +329,7 @@ __global__ __launch_bounds__(NT) void walk_kernel(const epara_verify_args* __res
     __syncthreads();
     if (tid == 0) {
         int n = 0;
-        for (int row = there ? 0 : s.rows; row < s.rows; row = lds.child[row]) lds.path[n++] = row;
+        for (int row = up == -1 ? 0 : s.rows; row < s.rows; row = lds.child[row]) lds.path[n++] = row;      // (up: the first row's; without that row no other is there)
         lds.kept = n;
         lds.eldest = INT32_MAX;
         lds.n_without = 0;
@@ -526,7 +531,7 @@ __global__ __launch_bounds__(NT) void draw_kernel(const drawn_row* __restrict__ 
     const double unit = d.unit, top_p = d.top_p, top_q = d.top_q;
     const float u = d.uniform;
     chunk_sum* sums = all_sums + static_cast<size_t>(i) * most_chunks;
-    double ratio = d.ratio, total = 0., goal = 0., base = 0.;
+    double ratio = d.ratio * MORE, total = 0., goal = 0., base = 0.;
     bool exact = false;                                    // the chunks' sums are of the very weights that pass 2 looks at
     // 0: my chunk's sums; 1: all chunks' once more, one after the other (only where next to nothing is left); 2: the chunk with the token
     for (int pass = 0;;) {
@@ -552,11 +557,10 @@ __global__ __launch_bounds__(NT) void draw_kernel(const drawn_row* __restrict__ 
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 const double b = exp2_64((static_cast<double>(x[j]) - top_q) * unit), left = out[j] - ratio * b;
-                const bool some_left = left > out[j] * SAME;
-                out[j] = some_left ? left : 0.;
+                out[j] = fmax(left, 0.);
                 sums_of[0] += out[j];
                 sums_of[2] += b;
-                sums_of[3] += some_left ? b : 0.;
+                sums_of[3] += left > 0. ? b : 0.;
             }
         }
         const double mine = sums_of[0];
@@ -588,16 +592,10 @@ __global__ __launch_bounds__(NT) void draw_kernel(const drawn_row* __restrict__ 
                 }
                 block_sums<2>(both, lds, before);
                 total = both[0];
-                move = total / both[1] - ratio;
+                move = total / both[1] * MORE - ratio;
                 ratio += move;
             }
-            // (a corrected sum is no more than the chunk's own sum with r; from 4 SAME of its weights on, some of them are over SAME themselves, and it has a token)
-            auto chunk_share = [&](int c) {
-                const double all = get_double(&sums[c].rest);
-                if (move == 0.) return all;
-                const double left = all - move * get_double(&sums[c].q_of_rest);
-                return left > get_double(&sums[c].p) * (4. * SAME) ? left : 0.;
-            };
+            auto chunk_share = [&](int c) { return move == 0. ? get_double(&sums[c].rest) : fmax(get_double(&sums[c].rest) - move * get_double(&sums[c].q_of_rest), 0.); };
             for (int c = lo; c < hi; ++c) some[0] += chunk_share(c);
             const double share_of_mine = some[0];
             block_sums<1>(some, lds, before);
@@ -631,7 +629,7 @@ __global__ __launch_bounds__(NT) void draw_kernel(const drawn_row* __restrict__ 
         }
         // ---- and the token in it
         const int found = block_find(base + before, mine, goal, lds);
-        if (found < 0) {                                   // (all threads; no call leaves without a token, whatever the sums were)
+        if (found < 0) {                                   // (all threads: a corrected sum that is rounding after all)
             if (exact) break;
             pass = 1;
             chunk = 0;

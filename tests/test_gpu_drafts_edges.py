@@ -1,8 +1,8 @@
 """GPU parity of verification where next to nothing is left to draw from: drafts that agree with the target but for a few tokens, over several chunks of a row, with the
 uniforms at the ends of their range.
 
-The sums and borders are compared as in test_gpu_drafts.py; here the oracle's weights are exactly those of the tokens that differ, since a difference under 2^-44 of a weight
-counts as none in both.  And trees whose first row is not there, of which nothing may stay, through every call of a step."""
+The sums and borders are compared as in test_gpu_drafts.py; here the oracle's weights are exactly those of the tokens that differ, since the draft's
+probabilities count 2^-44 more in both.  And trees whose first row is not there, of which nothing may stay, through every call of a step."""
 import numpy as np
 import pytest
 import torch
